@@ -75,12 +75,13 @@ def draw(rng):
     fill = rng.choice(["full", "ragged"])
     layout = rng.choice(["plain", "fused"])
     gain = rng.choice([0.25, 1.0, 2.0])
+    least = 2 if direction == "train" else 1       # (with one key the gradients of Q and K are zero: nothing to compare)
     if rng.random() < 0.55:
         Hk = log_int(1, 24)
         c = _cross("", direction, rng.choice([1, 1, 2, 3, 8]), Hk * rng.choice([1, 1, 2, 4]), Hk, log_int(1, 120000),
-                   log_int(1, 40000), d=d, dtype=dtype, fill=fill, layout=layout, gain=gain)
+                   log_int(least, 40000), d=d, dtype=dtype, fill=fill, layout=layout, gain=gain)
     else:
-        M = log_int(1, 6000)
+        M = log_int(least, 6000)
         step = rng.random() < 0.25
         buckets = rng.choice([8, 32, 64])
         c = _bias("", direction, rng.choice([1, 2, 3, 8]), log_int(1, 64), 1 if step else M, M, d=d, dtype=dtype, fill=fill,
@@ -101,7 +102,7 @@ def draw(rng):
             c["N"] = min(c["N"], c["M"])
             c["q_pos"] = c["M"] - 1 if c["q_pos"] else 0
         else:
-            c["N"], c["M"] = max(1, c["N"] // 2), max(1, c["M"] * 3 // 4)
+            c["N"], c["M"] = max(1, c["N"] // 2), max(least, c["M"] * 3 // 4)
     del c["name"]
     return c
 

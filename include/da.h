@@ -288,6 +288,85 @@ int da_sparse_attn_lists(const da_problem* p, const void* Qp, const void* Kp, co
 int da_forward_global(const da_problem* p, const void* Q, const void* K, const void* V, void* O, int32_t* row_ptr_out,
                       int32_t* cols_out, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Attention of N queries to M keys, every pair: what a text-conditioned transformer has next to the path above.  Per batch
+ * element b and head h of Q, with head h / (H / Hk) of K and V and the keys j < n_b (n_b = kv_len[b], or M):
+ *     x_ij = scale q_i.k_j (+ the bias of da_bias_attn)    lse_i = log sum_j exp x_ij    o_i = sum_j exp(x_ij - lse_i) v_j
+ * A key whose x is minus infinity weighs nothing; a row with nothing to attend (n_b = 0, or minus infinity throughout) has o = 0
+ * and lse = -inf, and its gradients are 0.
+ * K and V rows at or behind n_b are not read (they may hold anything) and get zero rows of dK and dV; kv_len outside [0, M] is
+ * brought into it.
+ */
+typedef struct da_attn_problem {
+  int32_t B, H, Hk;    /* batch, heads of Q and O, heads of K and V (H a multiple of Hk) */
+  int32_t N, M;        /* queries and keys (rows of K and V) of a batch element */
+  int32_t d;           /* head dimension: 64 or 128 */
+  int32_t dtype;       /* DA_F32 or DA_BF16: every tensor but lse and kv_len */
+  int32_t reserved;    /* 0 */
+  double  scale;       /* factor of the scores, > 0; 0 stands for 1/sqrt(d) */
+} da_attn_problem;
+
+/* Where the rows of each tensor live, [B, heads, rows, d] (see da_layout; every one has its own).  A da_layout of zeros, or NULL in the
+ * struct's place, means contiguous; the stride of an extent of 1 does not matter.  Rows of O, dQ, dK, dV must not overlap (DA_ERR_DIM).
+ * The forward calls check all of it and use q, k, v, o. */
+typedef struct da_attn_layouts {
+  da_layout q, k, v, o, dout, dq, dk, dv;
+} da_attn_layouts;
+
+/*
+ * The learned bias of text encoders of the T5 kind: table[bucket(r)][h] is added to the scaled score, r = j - (i + q_pos).
+ * A direction has n buckets: buckets / 2 if bidirectional (the upper half for r > 0, distance a = |r|), else all of them
+ * (a = -r, or 0 where the key lies ahead).  With e = n / 2 the bucket of a is a below e, and from there on
+ * e + floor((n - e) log(a / e) / log(max_distance / e)), at most n - 1; a distance on a border belongs to the bucket that begins there.
+ */
+typedef struct da_rel_bias {
+  int32_t buckets;       /* rows of the table: 2 .. 256 (bidirectional: 4 .. 256, even) */
+  int32_t max_distance;  /* n / 2 < max_distance <= 1024 */
+  int32_t bidirectional; /* 0 or 1 */
+  int32_t q_pos;         /* position of query 0 among the keys (0 for self attention, M - 1 for one new token behind the others) */
+} da_rel_bias;
+
+typedef struct da_attn_dims {
+  size_t forward_ws, backward_ws;  /* bytes of scratch (0: ws may be NULL) */
+} da_attn_dims;
+
+/* Host only, pure.  Scratch for da_cross_attn and da_cross_attn_bwd (bias NULL) or da_bias_attn and da_bias_attn_bwd.  It depends on the
+ * problem and the rule alone, not on layouts or lengths. */
+int da_attn_sizes(const da_attn_problem* p, const da_rel_bias* bias, da_attn_dims* out /* host */);
+
+/*
+ * Cross attention: queries Q [B,H,N,d] to an encoder's K, V [B,Hk,M,d], O [B,H,N,d].  kv_len [B] int32 (DEVICE, may be NULL: all M).
+ * lse [B,H,N] float, contiguous (may be NULL; the backward call needs it).  ws: da_attn_dims.forward_ws bytes, 256-byte aligned.
+ * Any N and M, from one query to sequences of hundreds of thousands: where there are few queries the keys are cut into pieces that
+ * are put together by a second launch.  bf16 uses bf16 matrix instructions with float32 accumulation, softmax and sums (probabilities
+ * enter the second product in bf16); f32 is float32 throughout.  The same call gives the same bits every time.
+ * d other than 64 or 128 returns DA_ERR_UNSUPPORTED.
+ */
+int da_cross_attn(const da_attn_problem* p, const da_attn_layouts* layouts, const void* Q, const void* K, const void* V,
+                  const int32_t* kv_len, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its gradients: dQ [B,H,N,d], dK, dV [B,Hk,M,d] (summed over the heads of Q that share them) of a loss whose gradient by O is dO [B,H,N,d].
+ * O and lse are those of the forward call; lse has no gradient of its own.  ws: da_attn_dims.backward_ws bytes, 256-byte aligned.
+ * No atomics: the same call gives the same bits every time.
+ */
+int da_cross_attn_bwd(const da_attn_problem* p, const da_attn_layouts* layouts, const void* Q, const void* K, const void* V,
+                      const int32_t* kv_len, const void* O, const float* lse, const void* dO, void* dQ, void* dK, void* dV, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/*
+ * Attention with the bias of da_rel_bias: table [buckets,H] in the problem's dtype, contiguous.  Everything else as da_cross_attn.
+ * Entries of -2^100 or less (minus infinity, the type's lowest value) mask their pairs.
+ */
+int da_bias_attn(const da_attn_problem* p, const da_rel_bias* bias, const da_attn_layouts* layouts, const void* Q, const void* K,
+                 const void* V, const void* table, const int32_t* kv_len, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Its gradients: those of da_cross_attn_bwd, and dtable [buckets,H] (the problem's dtype, summed in float32 over batch, queries and
+ * keys; zero for buckets that no pair has). */
+int da_bias_attn_bwd(const da_attn_problem* p, const da_rel_bias* bias, const da_attn_layouts* layouts, const void* Q, const void* K,
+                     const void* V, const void* table, const int32_t* kv_len, const void* O, const float* lse, const void* dO, void* dQ,
+                     void* dK, void* dV, void* dtable, void* ws, size_t ws_bytes, void* stream);
+
 /* Static string for a da_status value (never NULL). */
 const char* da_status_string(int status);
 

@@ -26,7 +26,8 @@ DA_STATIC_SCRATCH_BYTES = 32 << 20
 EXPORTS = ["da_derive", "da_workspace_size", "da_build_perm", "da_draft_map", "da_select_blocks",
            "da_permute", "da_sparse_attn", "da_forward", "da_forward_ex", "da_global_sizes", "da_select_blocks_global",
            "da_sparse_attn_lists", "da_forward_global", "da_sparse_attn_ex", "da_wait_failures",
-           "da_select_blocks_global_static", "da_status_string"]
+           "da_select_blocks_global_static", "da_attn_sizes", "da_cross_attn", "da_cross_attn_bwd", "da_bias_attn",
+           "da_bias_attn_bwd", "da_status_string"]
 
 
 class da_problem(ctypes.Structure):
@@ -48,6 +49,23 @@ class da_global_dims(ctypes.Structure):
 
 class da_layout(ctypes.Structure):
     _fields_ = [("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_n", ctypes.c_int64)]
+
+
+class da_attn_problem(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("N", ctypes.c_int32), ("M", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32), ("scale", ctypes.c_double)]
+
+
+class da_attn_layouts(ctypes.Structure):
+    _fields_ = [(n, da_layout) for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")]
+
+
+class da_rel_bias(ctypes.Structure):
+    _fields_ = [("buckets", ctypes.c_int32), ("max_distance", ctypes.c_int32), ("bidirectional", ctypes.c_int32), ("q_pos", ctypes.c_int32)]
+
+
+class da_attn_dims(ctypes.Structure):
+    _fields_ = [("forward_ws", ctypes.c_size_t), ("backward_ws", ctypes.c_size_t)]
 
 
 class DaError(RuntimeError):
@@ -85,6 +103,12 @@ def lib() -> ctypes.CDLL:
         L.da_forward_global.argtypes = [P, V, V, V, V, V, V, V, ctypes.c_size_t, V]
         L.da_sparse_attn_ex.argtypes = [P, V, V, V, V, V, V, ctypes.c_int, V, V]
         L.da_wait_failures.argtypes = [ctypes.POINTER(ctypes.c_uint64)]
+        A, Y, R, S = ctypes.POINTER(da_attn_problem), ctypes.POINTER(da_attn_layouts), ctypes.POINTER(da_rel_bias), ctypes.c_size_t
+        L.da_attn_sizes.argtypes = [A, R, ctypes.POINTER(da_attn_dims)]
+        L.da_cross_attn.argtypes = [A, Y, V, V, V, V, V, V, V, S, V]
+        L.da_cross_attn_bwd.argtypes = [A, Y, V, V, V, V, V, V, V, V, V, V, V, S, V]
+        L.da_bias_attn.argtypes = [A, R, Y, V, V, V, V, V, V, V, V, S, V]
+        L.da_bias_attn_bwd.argtypes = [A, R, Y, V, V, V, V, V, V, V, V, V, V, V, V, V, S, V]
         L.da_status_string.argtypes = [ctypes.c_int]
         L.da_status_string.restype = ctypes.c_char_p
         for name in EXPORTS[:-1]:
@@ -224,3 +248,99 @@ def da_wait_failures() -> int:
     n = ctypes.c_uint64(0)
     _check(lib().da_wait_failures(ctypes.byref(n)), "da_wait_failures")
     return int(n.value)
+
+
+def attn_problem(B, H, N, M, d, Hk=None, dtype=DA_BF16, scale=0.0) -> da_attn_problem:
+    return da_attn_problem(B, H, H if Hk is None else Hk, N, M, d, dtype, 0, float(scale))
+
+
+def rel_bias(buckets, max_distance, bidirectional=1, q_pos=0) -> da_rel_bias:
+    return da_rel_bias(buckets, max_distance, int(bidirectional), q_pos)
+
+
+def attn_layouts(q=None, k=None, v=None, o=None, do=None, dq=None, dk=None, dv=None) -> da_attn_layouts:
+    """da_layout of each tensor (layout_of); None: contiguous."""
+    return da_attn_layouts(*(x if x is not None else da_layout(0, 0, 0) for x in (q, k, v, o, do, dq, dk, dv)))
+
+
+def da_attn_sizes(p: da_attn_problem, bias: da_rel_bias = None) -> da_attn_dims:
+    out = da_attn_dims()
+    _check(lib().da_attn_sizes(ctypes.byref(p), ctypes.byref(bias) if bias is not None else None, ctypes.byref(out)), "da_attn_sizes")
+    return out
+
+
+_torch_dtypes = None
+
+
+def _place(t, what, name, shape, dtype, layout, device):
+    """Address of a tensor that is what the problem says it is (None and plain addresses: as they are)."""
+    if t is None or isinstance(t, int):
+        return t
+    ok = t.shape == shape and t.dtype is dtype and t.get_device() == device
+    if ok and layout is not None and (layout.stride_b or layout.stride_h or layout.stride_n):
+        want = (layout.stride_b, layout.stride_h, layout.stride_n, 1)
+        ok = all(n == 1 or a == b for n, a, b in zip(shape, t.stride(), want))
+    elif ok:
+        ok = t.is_contiguous()
+    if not ok:
+        raise DaError(-2, f"{what}: {name} is {tuple(t.shape)} of {t.dtype} on device {t.device}, strides {t.stride()}; expected "
+                          f"{tuple(shape)} of {dtype} on the current device, {device}, contiguous or as its layout says")
+    return t.data_ptr()
+
+
+def _attn(what, p, bias, layouts, Q, K, V, table, kv_len, O, lse, ws, stream, grads):
+    global _torch_dtypes
+    if _torch_dtypes is None:
+        import torch
+        _torch_dtypes = (torch, {DA_F32: torch.float32, DA_BF16: torch.bfloat16})
+    torch, dtypes = _torch_dtypes
+    L = lib()
+    dt = dtypes.get(p.dtype)
+    plain = isinstance(Q, int) or Q is None                       # plain addresses: nothing to look at
+    dev = -1 if plain else torch.cuda.current_device()
+    B, H, Hk, N, M, d = p.B, p.H, p.Hk, p.N, p.M, p.d
+    lq = lk = lv = lo = None
+    if layouts is not None:
+        lq, lk, lv, lo = layouts.q, layouts.k, layouts.v, layouts.o
+    rows, keys = (B, H, N, d), (B, Hk, M, d)
+    f32, i32 = torch.float32, torch.int32
+    q, k, v = _place(Q, what, "Q", rows, dt, lq, dev), _place(K, what, "K", keys, dt, lk, dev), _place(V, what, "V", keys, dt, lv, dev)
+    o, l = _place(O, what, "O", rows, dt, lo, dev), _place(lse, what, "lse", (B, H, N), f32, None, dev)
+    n = _place(kv_len, what, "kv_len", (B,), i32, None, dev)
+    ws_at, ws_bytes = (ws, 2 ** 63) if ws is None or isinstance(ws, int) else (ws.data_ptr(), ws.numel() * ws.element_size())
+    if ws is not None and not isinstance(ws, int) and not plain and ws.get_device() != dev:
+        raise DaError(-2, f"{what}: ws is on device {ws.device}, the current device is {dev}")
+    s = torch.cuda.current_stream().cuda_stream if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
+    P, Y = ctypes.byref(p), None if layouts is None else ctypes.byref(layouts)
+    R, shape = None, None
+    if bias is not None:
+        R, shape = ctypes.byref(bias), (bias.buckets, H)
+        table = _place(table, what, "table", shape, dt, None, dev)
+    if grads is None:
+        st = L.da_cross_attn(P, Y, q, k, v, n, o, l, ws_at, ws_bytes, s) if R is None else \
+            L.da_bias_attn(P, R, Y, q, k, v, table, n, o, l, ws_at, ws_bytes, s)
+    else:
+        names = (("dO", rows, "dout"), ("dQ", rows, "dq"), ("dK", keys, "dk"), ("dV", keys, "dv"))
+        g = [_place(t, what, m, sh, dt, None if layouts is None else getattr(layouts, a), dev) for t, (m, sh, a) in zip(grads, names)]
+        if R is None:
+            st = L.da_cross_attn_bwd(P, Y, q, k, v, n, o, l, *g, ws_at, ws_bytes, s)
+        else:
+            g.append(_place(grads[4], what, "dtable", shape, dt, None, dev))
+            st = L.da_bias_attn_bwd(P, R, Y, q, k, v, table, n, o, l, *g, ws_at, ws_bytes, s)
+    _check(st, what)
+
+
+def da_cross_attn(p, Q, K, V, O, ws, kv_len=None, lse=None, layouts=None, stream=None):
+    _attn("da_cross_attn", p, None, layouts, Q, K, V, None, kv_len, O, lse, ws, stream, None)
+
+
+def da_cross_attn_bwd(p, Q, K, V, O, lse, dO, dQ, dK, dV, ws, kv_len=None, layouts=None, stream=None):
+    _attn("da_cross_attn_bwd", p, None, layouts, Q, K, V, None, kv_len, O, lse, ws, stream, (dO, dQ, dK, dV))
+
+
+def da_bias_attn(p, bias, Q, K, V, table, O, ws, kv_len=None, lse=None, layouts=None, stream=None):
+    _attn("da_bias_attn", p, bias, layouts, Q, K, V, table, kv_len, O, lse, ws, stream, None)
+
+
+def da_bias_attn_bwd(p, bias, Q, K, V, table, O, lse, dO, dQ, dK, dV, dtable, ws, kv_len=None, layouts=None, stream=None):
+    _attn("da_bias_attn_bwd", p, bias, layouts, Q, K, V, table, kv_len, O, lse, ws, stream, (dO, dQ, dK, dV, dtable))

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(LIB_DIR, "libdraftattn.so")
 PROBE_LIB_PATH = os.path.join(LIB_DIR, "libdaprobe.so")
 
 SOURCES = ["da_api.hip", "k_permute.hip", "k_pool.hip", "k_draft.hip", "k_select.hip", "k_select_global.hip", "k_attn_f32.hip",
-           "k_attn_bf16_ring.hip"]
+           "k_attn_bf16_ring.hip", "da_dense_api.hip", "k_dense_fwd.hip", "k_dense_bwd.hip"]
 PROBE_SOURCES = ["probe/k_probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -28,16 +28,17 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 
 # files whose float32 results must be reproducible bit for bit on a CPU: no contraction
 STRICT_FP = {"k_pool.hip", "k_draft.hip"}
+MATRIX_RESULTS_IN_VGPRS = {"k_attn_bf16_ring.hip", "k_dense_fwd.hip", "k_dense_bwd.hip"}
 
 
 def _compile(src: str) -> str:
     obj = os.path.join(OBJ_DIR, os.path.splitext(os.path.basename(src))[0] + ".o")
     extra = ["-ffp-contract=off"] if src in STRICT_FP else []
-    if src == "k_attn_bf16_ring.hip":
+    if src in MATRIX_RESULTS_IN_VGPRS:
         # all MFMA results in ordinary vector registers: the softmax reads the scores many times, and the
         # state of 64 queries fits the 256 that a wave has at two waves per SIMD
         extra += ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-    if src == "k_attn_bf16_ring.hip":
+    if src in MATRIX_RESULTS_IN_VGPRS:
         extra.append("-fno-honor-nans")   # no NaN canonicalisation around max(); infinities stay exact
     cmd = [HIPCC, *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)

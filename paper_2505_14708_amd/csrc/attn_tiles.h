@@ -1,0 +1,316 @@
+// Tiles, operands and products that the dense attention kernels (k_dense_fwd.hip, k_dense_bwd.hip) share.
+//
+// A wave works on 32 columns at a time: 32 rows of one operand (queries, or keys in the kernel for the gradients of K and V), one to a
+// lane l % 32, that stay in registers, while tiles of rows of the others come through LDS.  Two products make up every kernel:
+//
+//   scores   C = X Y^T     X: 32 rows of an LDS tile, Y: the wave's 32 rows; contraction over the channels
+//   mix      Z += X^T C    X: the same kind of tile, read transposed; contraction over its 32 rows
+//
+// Lane l of the 64 holds in C's 16 registers the rows 16(a / 8) + 8(l / 32) + a % 8 of column l % 32 (a = 0..15): X's rows are fed in
+// the order sigma (bits 2 and 3 of the row number change places), so that 8 registers in a row are 8 rows in a row and C goes into
+// the second product without leaving its lane.  A softmax over rows of C is a lane's own registers and one exchange with lane l ^ 32.
+// Z's registers are the channels 32 dt + 8(a / 4) + 4(l / 32) + a % 4 of the same column.
+//
+// bf16: v_mfma_f32_32x32x16_bf16, X read in 16-byte pieces for the scores and by ds_read_b64_tr_b16 (four rows of 16 channels become
+// 16 columns of four) for the mix.  float32: v_mfma_f32_32x32x2_f32, a lane's 16-byte piece of X feeds four of them, and the mix reads
+// single words, whose transposition is a matter of addresses.
+//
+// Tiles are row major in LDS, 16-byte pieces of row r stored at piece number p ^ swizzle(r), and arrive by 16-byte direct-to-LDS loads: the
+// lane that fills position p of row r fetches piece p ^ swizzle(r).  The swizzles let both kinds of reads touch all banks.
+#pragma once
+#include <float.h>
+#include <math.h>
+#include "da_internal.h"
+#include "dense_attn.h"
+
+namespace da {
+namespace dense {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+typedef __attribute__((address_space(3))) float lds_f32;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <class T> struct Type;
+template <> struct Type<__bf16> {
+  typedef bf16x8 piece;
+  static constexpr int PER = 8;      // elements of a 16-byte piece
+};
+template <> struct Type<float> {
+  typedef f32x4 piece;
+  static constexpr int PER = 4;
+};
+
+template <class T, int D> constexpr int kRowBytes = D * (int)sizeof(T);
+
+template <class T, int D> __device__ __forceinline__ int swizzle(int row) {
+  if constexpr (sizeof(T) == 4) return row & 15;
+  else if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+  else return ((row & 2) << 1) | ((row >> 2) & 3);
+}
+
+__device__ __forceinline__ int sigma(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
+
+__device__ __forceinline__ f32x16 zero16() {
+  return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+}
+
+// 16 bytes a lane from global memory to LDS: lane i's land at lds + 16 i.  (m0 holds the LDS address; it is put back.)
+__device__ __forceinline__ void dma16(const void* g, unsigned lds) {
+  unsigned keep;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+      : "=&s"(keep) : "v"(g), "s"(lds) : "memory");
+}
+// the same with a uniform base and a 32-bit offset of the lane's own
+__device__ __forceinline__ void dma16(const void* base, unsigned off, unsigned lds) {
+  unsigned keep;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+      : "=&s"(keep) : "v"(off), "s"(base), "s"(lds) : "memory");
+}
+// 4 bytes a lane
+__device__ __forceinline__ void dma4(const void* g, unsigned lds) {
+  unsigned keep;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
+      : "=&s"(keep) : "v"(g), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// workgroup barrier behind which LDS written by the loads above may be read (each wave has waited for its own)
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+__device__ __forceinline__ float max_across_halves(float x) {
+  u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_across_halves(float x) {
+  u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ---------------------------------------------------------------------------------- tiles
+// ROWS rows of D elements, row j of the tile being row min(first + j, last) of `base` (rows `stride` bytes apart), into LDS at `lds`, by the NW
+// waves of the workgroup.  (Rows behind the last one repeat it: every address is one of a row that is there.)
+template <class T, int D, int ROWS, int NW>
+__device__ __forceinline__ void load_tile(const unsigned char* base, long long stride, int first, int last, unsigned lds, int wave, int lane) {
+  constexpr int RB = kRowBytes<T, D>, CPR = RB / 16, RPS = 64 / CPR, STEPS = ROWS / RPS;
+  static_assert(STEPS % NW == 0, "whole steps per wave");
+  const int r_in = lane / CPR, p = lane % CPR;
+  if (first + ROWS - 1 <= last && stride < (1LL << 24)) {
+    const unsigned char* at = base + (long long)first * stride;
+#pragma unroll
+    for (int k = 0; k < STEPS / NW; ++k) {
+      const int it = k * NW + wave, row = it * RPS + r_in;
+      dma16(at + (long long)(it * RPS) * stride, (unsigned)(r_in * (int)stride + ((p ^ swizzle<T, D>(row)) << 4)), lds + it * 1024);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < STEPS / NW; ++k) {
+      const int it = k * NW + wave, row = it * RPS + r_in;
+      dma16(base + (long long)min(first + row, last) * stride + ((p ^ swizzle<T, D>(row)) << 4), lds + it * 1024);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------- products
+// A wave's own 32 rows: piece 2t + l / 32 of row l % 32.
+template <class T, int D> struct Own {
+  static constexpr int N = kRowBytes<T, D> / 32;
+  typename Type<T>::piece x[N];
+  __device__ __forceinline__ void load(const unsigned char* row, int hi) {
+#pragma unroll
+    for (int t = 0; t < N; ++t) x[t] = *(const typename Type<T>::piece*)(row + (2 * t + hi) * 16);
+  }
+};
+
+// LDS address (less the tile's) of the piece that this lane feeds to step 0 of `scores`; that of step t is at ^ 32 t
+template <class T, int D> __device__ __forceinline__ unsigned scores_lane(int lane) {
+  const int row = sigma(lane & 31);
+  return row * kRowBytes<T, D> + (((lane >> 5) ^ swizzle<T, D>(row)) << 4);
+}
+
+// NQ sets of 32 columns against 32 rows of the tile
+template <class T, int D, int NQ>
+__device__ __forceinline__ void scores(unsigned at, const Own<T, D> (&own)[NQ], f32x16 (&c)[NQ]) {
+#pragma unroll
+  for (int h = 0; h < NQ; ++h) c[h] = zero16();
+#pragma unroll
+  for (int t = 0; t < Own<T, D>::N; ++t) {
+    if constexpr (sizeof(T) == 2) {
+      const bf16x8 x = *(lds_bf16x8*)(uintptr_t)(at ^ (32 * t));
+#pragma unroll
+      for (int h = 0; h < NQ; ++h) c[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, own[h].x[t], c[h], 0, 0, 0);
+    } else {
+      const f32x4 x = *(lds_f32x4*)(uintptr_t)(at ^ (32 * t));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < NQ; ++h) c[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], own[h].x[t][i], c[h], 0, 0, 0);
+    }
+  }
+}
+
+// LDS address (less the tile's) of this lane's part of the transposed operands: bf16: rows 8(l/32) + 0..3 of step 0, channel group 0; channel
+// group dt is at ^ 64 dt, step t 16 rows further, rows + 4: row + 4 and pieces ^ 1.  float32: row 8(l/32), channel l % 32.
+template <class T, int D> __device__ __forceinline__ unsigned mix_lane(int lane) {
+  const int hi = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    const int l = lane & 15, row = 8 * hi + (l >> 2), piece = 2 * ((lane >> 4) & 1) + ((l >> 1) & 1);
+    return row * kRowBytes<T, D> + ((piece ^ swizzle<T, D>(row)) << 4) + (l & 1) * 8;
+  } else {
+    const int m = lane & 31, row = 8 * hi;
+    return row * kRowBytes<T, D> + (((m >> 2) ^ swizzle<T, D>(row)) << 4) + (m & 3) * 4;
+  }
+}
+
+// c as the right operand of `mix`.  bf16: rounded to nearest; a probability or its gradient enters the product with 8 bits, as every bf16
+// operand does, and is summed in 32.
+template <class T> struct Mixed;
+template <> struct Mixed<__bf16> {
+  bf16x8 x[2];
+  __device__ __forceinline__ explicit Mixed(const f32x16& c) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bf16x2 p = __builtin_convertvector((f32x2{c[2 * i], c[2 * i + 1]}), bf16x2);
+      x[i >> 2][(2 * i) & 7] = p[0];
+      x[i >> 2][(2 * i + 1) & 7] = p[1];
+    }
+  }
+};
+template <> struct Mixed<float> {
+  f32x16 x;
+  __device__ __forceinline__ explicit Mixed(const f32x16& c) : x(c) {}
+};
+
+template <class T, int D, int NQ>
+__device__ __forceinline__ void mix(unsigned at, const Mixed<T> (&c)[NQ], f32x16 (&z)[NQ][D / 32]) {
+  constexpr int RB = kRowBytes<T, D>;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        const unsigned a0 = (at ^ (64 * dt)) + t * 16 * RB, a1 = (at ^ (64 * dt + 16)) + (t * 16 + 4) * RB;
+        const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a0);
+        const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a1);
+        const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int h = 0; h < NQ; ++h) z[h][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, c[h].x[t], z[h][dt], 0, 0, 0);
+      }
+  } else {
+#pragma unroll
+    for (int a = 0; a < 16; ++a)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        const unsigned w = (at ^ (((a & 7) << 4) | (dt << 7))) + (16 * (a >> 3) + (a & 7)) * RB;
+        const float x = *(lds_f32*)(uintptr_t)w;
+#pragma unroll
+        for (int h = 0; h < NQ; ++h) z[h][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, c[h].x[a], z[h][dt], 0, 0, 0);
+      }
+  }
+}
+
+// row of C that register a of a lane holds
+__device__ __forceinline__ int c_row(int a, int hi) { return 16 * (a >> 3) + 8 * hi + (a & 7); }
+
+// A column of Z (D channels of one row of the result) to its place, in the result's type: 16 bytes a lane where two lanes of a row
+// exchange halves first.
+template <class T, int D>
+__device__ __forceinline__ void store_column(unsigned char* row, int hi, const f32x16 (&z)[D / 32], float f, bool there) {
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{z[dt][8 * k + 2 * i] * f, z[dt][8 * k + 2 * i + 1] * f}), bf16x2));
+        // w[0..1]: channels 16k + 4hi + 0..3, w[2..3]: 16k + 8 + 4hi + 0..3; afterwards the lane has 16k + 8hi + 0..7
+        const u32x2 s0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const u32x2 s1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        if (there) *(u32x4*)(row + (32 * dt + 16 * k + 8 * hi) * 2) = u32x4{s0[0], s1[0], s0[1], s1[1]};
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (there)
+          *(f32x4*)(row + (32 * dt + 8 * k + 4 * hi) * 4) =
+              f32x4{z[dt][4 * k] * f, z[dt][4 * k + 1] * f, z[dt][4 * k + 2] * f, z[dt][4 * k + 3] * f};
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------- relative position bias
+// The bias of a head by r = key - query - q_pos, times log2(e), in LDS: r from -(cut + kBiasPad) to cut + kBiasPad, what lies beyond `cut`
+// having the outermost buckets' values.  A square of 32 x 32 that touches -cut < r < cut reaches no further than kBiasPad past it.
+constexpr int kBiasPad = 64;
+constexpr float kMasks = -0x1p100f;
+__host__ __device__ inline int bias_entries(int cut) { return 2 * (cut + kBiasPad) + 1; }
+
+template <class T>
+__device__ __forceinline__ void fill_bias(float* lds, const RelRule& rule, const T* table, int H, int h, int thread, int threads) {
+  const int n = bias_entries(rule.cut);
+  for (int i = thread; i < n; i += threads) {
+    const float b = (float)table[(long long)rel_bucket(rule, i - rule.cut - kBiasPad) * H + h];
+    // A mask of the type's lowest value is minus infinity here: beside numbers of that size a score leaves no trace, nor does log(sum) in
+    // lse, from which the backward pass could not make the probabilities again.
+    lds[i] = b <= kMasks ? -INFINITY : b * kLog2e;
+  }
+}
+
+// the swap of a table's registers for a square: where the wave's columns are queries (SIGN +1: r grows with the register's row) or keys (-1)
+template <int SIGN>
+__device__ __forceinline__ void read_bias(unsigned at, f32x16& b) {
+#pragma unroll
+  for (int a = 0; a < 16; ++a) b[a] = *(lds_f32*)(uintptr_t)(at + SIGN * 4 * (16 * (a >> 3) + (a & 7)));
+}
+
+// workgroups are dealt to the 8 XCDs in turn: consecutive pieces of work go to one XCD, whose L2 then holds the rows they share
+__device__ __forceinline__ long long xcd_order(long long id, long long total) {
+  const long long each = total / 8, more = total % 8, x = id % 8;
+  return x * each + min(x, more) + id / 8;
+}
+
+// rows of a tile: 16 KB of K and of V at most, so that two workgroups of two buffers fit a CU
+template <class T, int D> constexpr int kKeys = kRowBytes<T, D> > 256 ? 32 : 64;
+
+// where row rr of head `hd` (of those the kernels see) of batch element b lives
+template <bool BIAS>
+__device__ __forceinline__ long long query_offset(const DenseGeo& q, const Rows& r, int b, int hd, int rr) {
+  if constexpr (BIAS) return b * r.sb + hd * r.sh + (long long)rr * r.sn;
+  if (q.group == 1) return b * r.sb + hd * r.sh + (long long)rr * r.sn;
+  const int g = rr / q.N, n = rr - g * q.N;
+  return b * r.sb + (long long)(hd * q.group + g) * r.sh + (long long)n * r.sn;
+}
+
+}  // namespace dense
+
+constexpr int kCUs = 256;
+
+inline dim3 grid_of(long long n) {            // n workgroups of at most 256 threads, in as many rows as the limit of 2^32 threads along x makes
+  const long long x = n < (1LL << 23) ? n : (1LL << 23);
+  return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+
+}  // namespace da

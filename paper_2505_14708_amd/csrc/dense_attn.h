@@ -1,0 +1,38 @@
+// One problem of the dense attention kernels (attention to an encoder's states, attention with a relative position bias), host and device.
+#pragma once
+#include "da_internal.h"
+#include "rel_buckets.h"
+
+namespace da {
+
+struct DenseGeo {
+  int B, H, Hk, group, N, M, d, dtype;
+  float c2;              // scale * log2(e): the softmax works in powers of two
+  float scale;
+  Rows q, k, v, o, dout, dq, dk, dv;
+  const int32_t* kv_len; // keys of each batch element (NULL: M)
+  // with a bias
+  int bias, buckets, q_pos;
+  RelRule rule;
+};
+
+// Rows of queries as the kernels see them.  Without a bias the queries of all heads that share a head of K and V are one list (queries of
+// one position in several heads fill a tile); with a bias, which is per head, each head has its own.
+inline int dense_heads(const DenseGeo& q) { return q.bias ? q.H : q.Hk; }
+inline long long dense_rows(const DenseGeo& q) { return q.bias ? q.N : (long long)q.group * q.N; }
+
+// How the work is cut (host rule; the reasons stand at the functions)
+struct FwdPlan {
+  int waves, sets;       // waves of a workgroup, sets of 32 queries of a wave
+  int tiles, splits;     // tiles of queries of a head, pieces of the keys
+};
+FwdPlan plan_dense_fwd(const DenseGeo& q);
+size_t dense_fwd_workspace(const DenseGeo& q);
+size_t dense_bwd_workspace(const DenseGeo& q);
+
+hipError_t launch_dense_fwd(const DenseGeo& q, const void* Q, const void* K, const void* V, const void* table, void* O, float* lse,
+                            void* ws, hipStream_t s);
+hipError_t launch_dense_bwd(const DenseGeo& q, const void* Q, const void* K, const void* V, const void* table, const void* O,
+                            const float* lse, const void* dO, void* dQ, void* dK, void* dV, void* dtable, void* ws, hipStream_t s);
+
+}  // namespace da

@@ -1,0 +1,257 @@
+// Dense attention of N queries to M keys, forward: softmax(scale Q K^T + bias) V in one pass over the keys.
+//
+// Per set of 32 queries and 32 keys a wave computes S^T = K Q^T, the running maximum and sum of the softmax, and O^T += V^T P^T, with the
+// two products of attn_tiles.h; the queries lie on the lane axis.  Tiles of K and V come through LDS, twice buffered and shared by the waves
+// of the workgroup.
+#include "attn_tiles.h"
+
+namespace da {
+namespace dense {
+
+constexpr float kLazy = 8.0f;          // the reference of the exponentials moves when a score exceeds it by more than this many powers of two
+
+struct FwdArgs {
+  const unsigned char *Q, *K, *V;
+  const void* table;
+  unsigned char* O;
+  float* lse;
+  float* part;           // splits > 1: [work item][rows of the tile][D] sums of P V, then [work item][rows of the tile][2] reference and sum of P
+  int tiles, splits;
+  long long rows, items; // queries of a head, work items
+};
+
+template <class T, int D, int NQ, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(DenseGeo q, FwdArgs g) {
+  constexpr int KB = kKeys<T, D>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * NQ * NW;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * TILE];   // K, V, K, V
+  extern __shared__ __attribute__((aligned(16))) float bias_row[];
+  const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
+  if (id >= g.items) return;
+  const long long item = xcd_order(id, g.items);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
+  const int split = (int)(item % g.splits);
+  const long long bht = item / g.splits;
+  const int tile = (int)(bht % g.tiles);
+  const long long bh = bht / g.tiles;
+  const int heads = BIAS ? q.H : q.Hk;
+  const int b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads), hk = BIAS ? hd / q.group : hd;
+  const int len = q.kv_len ? min(max(q.kv_len[b], 0), q.M) : q.M;
+  const int first_row = tile * RT + wave * (32 * NQ), last_row = (int)g.rows - 1;
+
+  // this split's keys
+  const int n_tiles = (len + KB - 1) / KB, each = (n_tiles + g.splits - 1) / g.splits;
+  const int t0 = min(split * each, n_tiles), t1 = min(t0 + each, n_tiles);
+  const long long ks = q.k.sn * (long long)sizeof(T), vs = q.v.sn * (long long)sizeof(T);
+  const unsigned char* kb = g.K + (b * q.k.sb + hk * q.k.sh) * (long long)sizeof(T);
+  const unsigned char* vb = g.V + (b * q.v.sb + hk * q.v.sh) * (long long)sizeof(T);
+  const unsigned lds = (unsigned)(uintptr_t)(lds_f32*)tiles;
+  if (t0 < t1) {
+    load_tile<T, D, KB, NW>(kb, ks, t0 * KB, len - 1, lds, wave, lane);
+    load_tile<T, D, KB, NW>(vb, vs, t0 * KB, len - 1, lds + TILE, wave, lane);
+  }
+  if constexpr (BIAS) fill_bias<T>(bias_row, q.rule, (const T*)g.table, q.H, hd, threadIdx.x, 64 * NW);
+
+  Own<T, D> own[NQ];
+  f32x16 z[NQ][D / 32];
+  float ref[NQ], sum[NQ];
+#pragma unroll
+  for (int h = 0; h < NQ; ++h) {
+    own[h].load(g.Q + query_offset<BIAS>(q, q.q, b, hd, min(first_row + 32 * h + (lane & 31), last_row)) * (long long)sizeof(T), hi);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) z[h][dt] = zero16();
+    // below every finite score, so that scores of minus infinity weigh nothing from the start
+    ref[h] = -FLT_MAX;
+    sum[h] = 0.f;
+  }
+  const unsigned s_lane = scores_lane<T, D>(lane), m_lane = mix_lane<T, D>(lane);
+  const unsigned bias_lds = BIAS ? (unsigned)(uintptr_t)(lds_f32*)bias_row : 0u;
+
+  for (int t = t0; t < t1; ++t) {
+    const unsigned buf = lds + ((t - t0) & 1) * (2 * TILE);
+    wait_loads();
+    tile_barrier();
+    if (t + 1 < t1) {
+      const unsigned next = lds + ((t + 1 - t0) & 1) * (2 * TILE);
+      load_tile<T, D, KB, NW>(kb, ks, (t + 1) * KB, len - 1, next, wave, lane);
+      load_tile<T, D, KB, NW>(vb, vs, (t + 1) * KB, len - 1, next + TILE, wave, lane);
+    }
+    if (NW > 1 && first_row > last_row) continue;      // (a wave of padding only helps to load)
+#pragma unroll
+    for (int sub = 0; sub < KB / 32; ++sub) {
+      const int key0 = t * KB + 32 * sub;
+      if (key0 >= len) break;
+      f32x16 s[NQ];
+      scores<T, D, NQ>(buf + sub * 32 * RB + s_lane, own, s);
+      float mx[NQ];
+      bool moves = false;
+      const int left = len - key0 - 8 * hi;
+#pragma unroll
+      for (int h = 0; h < NQ; ++h) {
+        if constexpr (BIAS) {
+          const int low = key0 - (first_row + 32 * h) - q.q_pos;          // r of key 0 and query 0 of the square
+          if (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut) {
+            const float far = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
+#pragma unroll
+            for (int a = 0; a < 16; ++a) s[h][a] = __builtin_fmaf(s[h][a], q.c2, far);
+          } else {
+            f32x16 bs;
+            read_bias<1>(bias_lds + 4 * (low + 8 * hi - (lane & 31) + q.rule.cut + kBiasPad), bs);
+#pragma unroll
+            for (int a = 0; a < 16; ++a) s[h][a] = __builtin_fmaf(s[h][a], q.c2, bs[a]);
+          }
+        }
+        if (key0 + 32 > len) {
+#pragma unroll
+          for (int a = 0; a < 16; ++a) s[h][a] = 16 * (a >> 3) + (a & 7) < left ? s[h][a] : -INFINITY;
+        }
+        float m = s[h][0];
+#pragma unroll
+        for (int a = 1; a < 16; ++a) m = fmaxf(m, s[h][a]);
+        m = max_across_halves(m);
+        mx[h] = BIAS ? m : m * q.c2;
+        moves = moves || mx[h] - ref[h] > kLazy;
+      }
+      if (__any(moves)) {
+#pragma unroll
+        for (int h = 0; h < NQ; ++h) {
+          const float to = fmaxf(ref[h], mx[h]), f = exp2_fast(ref[h] - to);
+          ref[h] = to;
+          sum[h] *= f;
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int a = 0; a < 16; ++a) z[h][dt][a] *= f;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < NQ; ++h) {
+#pragma unroll
+        for (int a = 0; a < 16; ++a) {
+          s[h][a] = exp2_fast(BIAS ? s[h][a] - ref[h] : __builtin_fmaf(s[h][a], q.c2, -ref[h]));
+          sum[h] += s[h][a];
+        }
+      }
+      if constexpr (NQ == 1) {
+        const Mixed<T> p[1] = {Mixed<T>(s[0])};
+        mix<T, D, 1>(buf + TILE + sub * 32 * RB + m_lane, p, z);
+      } else {
+        const Mixed<T> p[2] = {Mixed<T>(s[0]), Mixed<T>(s[1])};
+        mix<T, D, 2>(buf + TILE + sub * 32 * RB + m_lane, p, z);
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < NQ; ++h) {
+    const int rr = first_row + 32 * h + (lane & 31);
+    const bool there = rr <= last_row;
+    const float l = sum_across_halves(sum[h]);
+    if (g.splits == 1) {
+      const int rc = min(rr, last_row);
+      store_column<T, D>(g.O + query_offset<BIAS>(q, q.o, b, hd, rc) * (long long)sizeof(T), hi, z[h], l > 0.f ? 1.f / l : 0.f, there);
+      if (g.lse && there && hi == 0) g.lse[bh * g.rows + rr] = l > 0.f ? (ref[h] + __log2f(l)) * kLn2 : -INFINITY;
+    } else {
+      const long long at = item * RT + wave * (32 * NQ) + 32 * h + (lane & 31);
+      store_column<float, D>((unsigned char*)(g.part + at * D), hi, z[h], 1.f, there);
+      if (there && hi == 0) *(f32x2*)(g.part + g.items * RT * D + at * 2) = f32x2{ref[h], l};
+    }
+  }
+}
+
+// The pieces of a row put together: a wave for each row, in the order of the pieces.
+template <class T, int D, bool BIAS>
+__global__ __launch_bounds__(256) void dense_join_kernel(DenseGeo q, FwdArgs g, int RT) {
+  const long long row = (blockIdx.y * (long long)gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int heads = BIAS ? q.H : q.Hk;
+  if (row >= (long long)q.B * heads * g.rows) return;
+  const long long bh = row / g.rows;
+  const int rr = (int)(row - bh * g.rows), b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads);
+  const int tile = rr / RT;
+  const long long first = ((bh * g.tiles + tile) * g.splits) * RT + (rr - tile * RT);
+  const float* stat = g.part + g.items * RT * D;
+  float top = -FLT_MAX;
+  for (int s = 0; s < g.splits; ++s) {
+    const f32x2 x = *(const f32x2*)(stat + (first + (long long)s * RT) * 2);
+    if (x[1] > 0.f) top = fmaxf(top, x[0]);
+  }
+  constexpr int E = D / 64;
+  float o[E] = {}, l = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < g.splits; ++s) {
+    const f32x2 x = *(const f32x2*)(stat + (first + (long long)s * RT) * 2);
+    const float f = x[1] > 0.f ? exp2_fast(x[0] - top) : 0.f;
+    l = __builtin_fmaf(x[1], f, l);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(g.part[(first + (long long)s * RT) * D + lane * E + e], f, o[e]);
+  }
+  T* out = (T*)g.O + query_offset<BIAS>(q, q.o, b, hd, rr);
+#pragma unroll
+  for (int e = 0; e < E; ++e) out[lane * E + e] = (T)(l > 0.f ? o[e] / l : 0.f);
+  if (g.lse && lane == 0) g.lse[row] = l > 0.f ? (top + __log2f(l)) * kLn2 : -INFINITY;
+}
+
+}  // namespace dense
+
+namespace {
+
+template <class T, int D, int NQ, int NW, bool BIAS>
+hipError_t run_fwd(const DenseGeo& q, const FwdPlan& p, dense::FwdArgs a, hipStream_t s) {
+  const size_t lds = BIAS ? dense::bias_entries(q.rule.cut) * sizeof(float) : 0;
+  dense::dense_fwd_kernel<T, D, NQ, NW, BIAS><<<grid_of(a.items), 64 * NW, lds, s>>>(q, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const long long rows = (long long)q.B * dense_heads(q) * a.rows;
+  dense::dense_join_kernel<T, D, BIAS><<<grid_of((rows + 3) / 4), 256, 0, s>>>(q, a, 32 * NQ * NW);
+  return hipGetLastError();
+}
+
+template <class T, int D, bool BIAS>
+hipError_t pick_fwd(const DenseGeo& q, const FwdPlan& p, const dense::FwdArgs& a, hipStream_t s) {
+  if (p.waves == 1) return run_fwd<T, D, 1, 1, BIAS>(q, p, a, s);
+  if (p.sets == 1) return run_fwd<T, D, 1, 4, BIAS>(q, p, a, s);
+  if constexpr (sizeof(T) == 2) return run_fwd<T, D, 2, 4, BIAS>(q, p, a, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+FwdPlan plan_dense_fwd(const DenseGeo& q) {
+  FwdPlan p;
+  const long long rows = dense_rows(q), bh = (long long)q.B * dense_heads(q);
+  p.waves = rows <= 64 ? 1 : 4;
+  p.sets = q.dtype == DA_BF16 && p.waves == 4 && bh * ((rows + 255) / 256) >= kCUs ? 2 : 1;
+  const int rt = 32 * p.sets * p.waves;
+  p.tiles = (int)((rows + rt - 1) / rt);
+  const int kb = q.dtype == DA_F32 && q.d == 128 ? 32 : 64;
+  const long long wgs = bh * p.tiles, key_tiles = (q.M + kb - 1) / kb, want = p.waves == 1 ? 4 * kCUs : 2 * kCUs;
+  long long splits = wgs >= want ? 1 : (want + wgs - 1) / wgs;
+  if (splits > key_tiles / 4) splits = key_tiles / 4;
+  p.splits = splits < 1 ? 1 : (int)splits;
+  return p;
+}
+
+size_t dense_fwd_workspace(const DenseGeo& q) {
+  const FwdPlan p = plan_dense_fwd(q);
+  if (p.splits == 1) return 0;
+  return (size_t)q.B * dense_heads(q) * p.tiles * p.splits * (32 * p.sets * p.waves) * (q.d + 2) * sizeof(float);
+}
+
+hipError_t launch_dense_fwd(const DenseGeo& q, const void* Q, const void* K, const void* V, const void* table, void* O, float* lse,
+                            void* ws, hipStream_t s) {
+  const FwdPlan p = plan_dense_fwd(q);
+  dense::FwdArgs a;
+  a.Q = (const unsigned char*)Q; a.K = (const unsigned char*)K; a.V = (const unsigned char*)V;
+  a.table = table; a.O = (unsigned char*)O; a.lse = lse; a.part = (float*)ws;
+  a.tiles = p.tiles; a.splits = p.splits;
+  a.rows = dense_rows(q);
+  a.items = (long long)q.B * dense_heads(q) * p.tiles * p.splits;
+  const bool bias = q.bias != 0;
+  if (q.dtype == DA_BF16) {
+    if (q.d == 128) return bias ? pick_fwd<__bf16, 128, true>(q, p, a, s) : pick_fwd<__bf16, 128, false>(q, p, a, s);
+    return bias ? pick_fwd<__bf16, 64, true>(q, p, a, s) : pick_fwd<__bf16, 64, false>(q, p, a, s);
+  }
+  if (q.d == 128) return bias ? pick_fwd<float, 128, true>(q, p, a, s) : pick_fwd<float, 128, false>(q, p, a, s);
+  return bias ? pick_fwd<float, 64, true>(q, p, a, s) : pick_fwd<float, 64, false>(q, p, a, s);
+}
+
+}  // namespace da

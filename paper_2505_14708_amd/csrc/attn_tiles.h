@@ -91,6 +91,14 @@ __device__ __forceinline__ void dma4(const void* g, unsigned lds) {
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// the lane number, in a way that the compiler neither moves nor keeps: what follows from it is made anew in each trip of a loop, where
+// registers are short
+__device__ __forceinline__ int opaque_lane() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
 // workgroup barrier behind which LDS written by the loads above may be read (each wave has waited for its own)
 __device__ __forceinline__ void tile_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -112,9 +120,10 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // ROWS rows of D elements, row j of the tile being row min(first + j, last) of `base` (rows `stride` bytes apart), into LDS at `lds`, by the NW
 // waves of the workgroup.  (Rows behind the last one repeat it: every address is one of a row that is there.)
 template <class T, int D, int ROWS, int NW>
-__device__ __forceinline__ void load_tile(const unsigned char* base, long long stride, int first, int last, unsigned lds, int wave, int lane) {
+__device__ __forceinline__ void load_tile(const unsigned char* base, long long stride, int first, int last, unsigned lds, int wave) {
   constexpr int RB = kRowBytes<T, D>, CPR = RB / 16, RPS = 64 / CPR, STEPS = ROWS / RPS;
   static_assert(STEPS % NW == 0, "whole steps per wave");
+  const int lane = opaque_lane();
   const int r_in = lane / CPR, p = lane % CPR;
   if (first + ROWS - 1 <= last && stride < (1LL << 24)) {
     const unsigned char* at = base + (long long)first * stride;
@@ -149,25 +158,37 @@ template <class T, int D> __device__ __forceinline__ unsigned scores_lane(int la
   return row * kRowBytes<T, D> + (((lane >> 5) ^ swizzle<T, D>(row)) << 4);
 }
 
-// NQ sets of 32 columns against 32 rows of the tile
+// NQ sets of 32 columns against 32 rows of the tile, added to what c holds
+template <class T, int D, int NQ>
+__device__ __forceinline__ void add_scores(unsigned at, const Own<T, D> (&own)[NQ], f32x16 (&c)[NQ]) {
+  // operands arrive AHEAD steps before their use and no earlier: more of them in flight would not fit the registers
+  constexpr int N = Own<T, D>::N, AHEAD = 3;
+  typename Type<T>::piece x[N];
+  auto fetch = [&](int t) { x[t] = *(const __attribute__((address_space(3))) typename Type<T>::piece*)(uintptr_t)(at ^ (32 * t)); };
+#pragma unroll
+  for (int t = 0; t < AHEAD; ++t) fetch(t);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    if (t + AHEAD < N) fetch(t + AHEAD);
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int h = 0; h < NQ; ++h) c[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[t], own[h].x[t], c[h], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < NQ; ++h) c[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[t][i], own[h].x[t][i], c[h], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 template <class T, int D, int NQ>
 __device__ __forceinline__ void scores(unsigned at, const Own<T, D> (&own)[NQ], f32x16 (&c)[NQ]) {
 #pragma unroll
   for (int h = 0; h < NQ; ++h) c[h] = zero16();
-#pragma unroll
-  for (int t = 0; t < Own<T, D>::N; ++t) {
-    if constexpr (sizeof(T) == 2) {
-      const bf16x8 x = *(lds_bf16x8*)(uintptr_t)(at ^ (32 * t));
-#pragma unroll
-      for (int h = 0; h < NQ; ++h) c[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, own[h].x[t], c[h], 0, 0, 0);
-    } else {
-      const f32x4 x = *(lds_f32x4*)(uintptr_t)(at ^ (32 * t));
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int h = 0; h < NQ; ++h) c[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], own[h].x[t][i], c[h], 0, 0, 0);
-    }
-  }
+  add_scores<T, D, NQ>(at, own, c);
 }
 
 // LDS address (less the tile's) of this lane's part of the transposed operands: bf16: rows 8(l/32) + 0..3 of step 0, channel group 0; channel
@@ -188,6 +209,7 @@ template <class T, int D> __device__ __forceinline__ unsigned mix_lane(int lane)
 template <class T> struct Mixed;
 template <> struct Mixed<__bf16> {
   bf16x8 x[2];
+  Mixed() = default;
   __device__ __forceinline__ explicit Mixed(const f32x16& c) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -199,34 +221,46 @@ template <> struct Mixed<__bf16> {
 };
 template <> struct Mixed<float> {
   f32x16 x;
+  Mixed() = default;
   __device__ __forceinline__ explicit Mixed(const f32x16& c) : x(c) {}
 };
 
 template <class T, int D, int NQ>
 __device__ __forceinline__ void mix(unsigned at, const Mixed<T> (&c)[NQ], f32x16 (&z)[NQ][D / 32]) {
-  constexpr int RB = kRowBytes<T, D>;
+  constexpr int RB = kRowBytes<T, D>, G = D / 32;
   if constexpr (sizeof(T) == 2) {
+    constexpr int N = 2 * G, AHEAD = 3;
+    s16x8 x[N];
+    auto fetch = [&](int i) {
+      const int t = i / G, dt = i % G;
+      const unsigned a0 = (at ^ (64 * dt)) + t * 16 * RB, a1 = (at ^ (64 * dt + 16)) + (t * 16 + 4) * RB;
+      const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a0);
+      const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a1);
+      x[i] = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int i = 0; i < AHEAD; ++i) fetch(i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) {
-        const unsigned a0 = (at ^ (64 * dt)) + t * 16 * RB, a1 = (at ^ (64 * dt + 16)) + (t * 16 + 4) * RB;
-        const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a0);
-        const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a1);
-        const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
+    for (int i = 0; i < N; ++i) {
+      if (i + AHEAD < N) fetch(i + AHEAD);
 #pragma unroll
-        for (int h = 0; h < NQ; ++h) z[h][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, c[h].x[t], z[h][dt], 0, 0, 0);
-      }
+      for (int h = 0; h < NQ; ++h)
+        z[h][i % G] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[i]), c[h].x[i / G], z[h][i % G], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   } else {
 #pragma unroll
-    for (int a = 0; a < 16; ++a)
+    for (int a = 0; a < 16; ++a) {
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) {
+      for (int dt = 0; dt < G; ++dt) {
         const unsigned w = (at ^ (((a & 7) << 4) | (dt << 7))) + (16 * (a >> 3) + (a & 7)) * RB;
         const float x = *(lds_f32*)(uintptr_t)w;
 #pragma unroll
         for (int h = 0; h < NQ; ++h) z[h][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, c[h].x[a], z[h][dt], 0, 0, 0);
       }
+      if (a % 2) __builtin_amdgcn_sched_barrier(0);
+    }
   }
 }
 
@@ -295,14 +329,25 @@ __device__ __forceinline__ long long xcd_order(long long id, long long total) {
 // rows of a tile: 16 KB of K and of V at most, so that two workgroups of two buffers fit a CU
 template <class T, int D> constexpr int kKeys = kRowBytes<T, D> > 256 ? 32 : 64;
 
+// What a launch is made for: its queries' rows are those of single heads, the same with a bias, or those of several heads (dense_packed).
+enum Mode { PLAIN, BIAS, PACKED };
+template <int MODE> __device__ __forceinline__ int heads_of(const DenseGeo& q) { return MODE == PACKED ? q.Hk : q.H; }
+template <int MODE> __device__ __forceinline__ int kv_head(const DenseGeo& q, int hd) { return MODE == PACKED || q.group == 1 ? hd : hd / q.group; }
+
 // where row rr of head `hd` (of those the kernels see) of batch element b lives
-template <bool BIAS>
+template <int MODE>
 __device__ __forceinline__ long long query_offset(const DenseGeo& q, const Rows& r, int b, int hd, int rr) {
-  if constexpr (BIAS) return b * r.sb + hd * r.sh + (long long)rr * r.sn;
-  if (q.group == 1) return b * r.sb + hd * r.sh + (long long)rr * r.sn;
+  if constexpr (MODE != PACKED) return b * r.sb + hd * r.sh + (long long)rr * r.sn;
   const int g = rr / q.N, n = rr - g * q.N;
   return b * r.sb + (long long)(hd * q.group + g) * r.sh + (long long)n * r.sn;
 }
+
+// s c2 + add.  float32: the rounding of c2 alone would be off by |s c2| 2^-25, and is made good.
+template <class T> __device__ __forceinline__ float biased(const DenseGeo& q, float s, float add) {
+  if constexpr (sizeof(T) == 4) add = __builtin_fmaf(s == -INFINITY ? 0.f : s, q.c2_lo, add);
+  return __builtin_fmaf(s, q.c2, add);
+}
+template <class T> __device__ __forceinline__ float power_of(const DenseGeo& q, float s, float add) { return exp2_fast(biased<T>(q, s, add)); }
 
 }  // namespace dense
 

@@ -58,6 +58,7 @@ int check_attn(const da_attn_problem* p, const da_rel_bias* bias, const da_attn_
   const double scale = p->scale > 0.0 ? p->scale : 1.0 / sqrt((double)p->d);
   q.scale = (float)scale;
   q.c2 = (float)(scale * 1.4426950408889634);
+  q.c2_lo = (float)(scale * 1.4426950408889634 - (double)q.c2);
   q.kv_len = nullptr;
   q.bias = 0; q.buckets = 0; q.q_pos = 0;
   q.rule = RelRule();

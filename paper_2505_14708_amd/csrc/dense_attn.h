@@ -7,7 +7,7 @@ namespace da {
 
 struct DenseGeo {
   int B, H, Hk, group, N, M, d, dtype;
-  float c2;              // scale * log2(e): the softmax works in powers of two
+  float c2, c2_lo;       // scale * log2(e), and what its rounding left: the softmax works in powers of two
   float scale;
   Rows q, k, v, o, dout, dq, dk, dv;
   const int32_t* kv_len; // keys of each batch element (NULL: M)
@@ -16,10 +16,13 @@ struct DenseGeo {
   RelRule rule;
 };
 
-// Rows of queries as the kernels see them.  Without a bias the queries of all heads that share a head of K and V are one list (queries of
-// one position in several heads fill a tile); with a bias, which is per head, each head has its own.
-inline int dense_heads(const DenseGeo& q) { return q.bias ? q.H : q.Hk; }
-inline long long dense_rows(const DenseGeo& q) { return q.bias ? q.N : (long long)q.group * q.N; }
+// Rows of queries as the kernels see them: each head's own, or, where heads share keys and have few queries each, those of all heads that share
+// a head of K and V as one list (queries of one position in several heads fill a tile, and K and V are read once for them).  A bias is per
+// head, so its queries stay apart; from kPackBelow queries on a head fills its tiles by itself.
+constexpr int kPackBelow = 256;
+inline bool dense_packed(const DenseGeo& q) { return !q.bias && q.group > 1 && q.N < kPackBelow; }
+inline int dense_heads(const DenseGeo& q) { return dense_packed(q) ? q.Hk : q.H; }
+inline long long dense_rows(const DenseGeo& q) { return dense_packed(q) ? (long long)q.group * q.N : q.N; }
 
 // How the work is cut (host rule; the reasons stand at the functions)
 struct FwdPlan {

@@ -3,6 +3,7 @@
 // Per set of 32 queries and 32 keys a wave computes S^T = K Q^T, the running maximum and sum of the softmax, and O^T += V^T P^T, with the
 // two products of attn_tiles.h; the queries lie on the lane axis.  Tiles of K and V come through LDS, twice buffered and shared by the waves
 // of the workgroup.
+#include <type_traits>
 #include "attn_tiles.h"
 
 namespace da {
@@ -20,7 +21,13 @@ struct FwdArgs {
   long long rows, items; // queries of a head, work items
 };
 
-template <class T, int D, int NQ, int NW, bool BIAS>
+// natural log of 2^ref l
+__device__ __forceinline__ float log_sum(float ref, float l) {
+  constexpr float kLn2Lo = 0.6931471805599453 - (double)kLn2;
+  return l > 0.f ? __builtin_fmaf(ref, kLn2, __builtin_fmaf(ref, kLn2Lo, logf(l))) : -INFINITY;
+}
+
+template <class T, int D, int NQ, int NW, int MODE>
 __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(DenseGeo q, FwdArgs g) {
   constexpr int KB = kKeys<T, D>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * NQ * NW;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * TILE];   // K, V, K, V
@@ -33,8 +40,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
   const long long bht = item / g.splits;
   const int tile = (int)(bht % g.tiles);
   const long long bh = bht / g.tiles;
-  const int heads = BIAS ? q.H : q.Hk;
-  const int b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads), hk = BIAS ? hd / q.group : hd;
+  const int heads = heads_of<MODE>(q);
+  const int b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads), hk = kv_head<MODE>(q, hd);
   const int len = q.kv_len ? min(max(q.kv_len[b], 0), q.M) : q.M;
   const int first_row = tile * RT + wave * (32 * NQ), last_row = (int)g.rows - 1;
 
@@ -46,17 +53,17 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
   const unsigned char* vb = g.V + (b * q.v.sb + hk * q.v.sh) * (long long)sizeof(T);
   const unsigned lds = (unsigned)(uintptr_t)(lds_f32*)tiles;
   if (t0 < t1) {
-    load_tile<T, D, KB, NW>(kb, ks, t0 * KB, len - 1, lds, wave, lane);
-    load_tile<T, D, KB, NW>(vb, vs, t0 * KB, len - 1, lds + TILE, wave, lane);
+    load_tile<T, D, KB, NW>(kb, ks, t0 * KB, len - 1, lds, wave);
+    load_tile<T, D, KB, NW>(vb, vs, t0 * KB, len - 1, lds + TILE, wave);
   }
-  if constexpr (BIAS) fill_bias<T>(bias_row, q.rule, (const T*)g.table, q.H, hd, threadIdx.x, 64 * NW);
+  if constexpr (MODE == BIAS) fill_bias<T>(bias_row, q.rule, (const T*)g.table, q.H, hd, threadIdx.x, 64 * NW);
 
   Own<T, D> own[NQ];
   f32x16 z[NQ][D / 32];
   float ref[NQ], sum[NQ];
 #pragma unroll
   for (int h = 0; h < NQ; ++h) {
-    own[h].load(g.Q + query_offset<BIAS>(q, q.q, b, hd, min(first_row + 32 * h + (lane & 31), last_row)) * (long long)sizeof(T), hi);
+    own[h].load(g.Q + query_offset<MODE>(q, q.q, b, hd, min(first_row + 32 * h + (lane & 31), last_row)) * (long long)sizeof(T), hi);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) z[h][dt] = zero16();
     // below every finite score, so that scores of minus infinity weigh nothing from the start
@@ -64,7 +71,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
     sum[h] = 0.f;
   }
   const unsigned s_lane = scores_lane<T, D>(lane), m_lane = mix_lane<T, D>(lane);
-  const unsigned bias_lds = BIAS ? (unsigned)(uintptr_t)(lds_f32*)bias_row : 0u;
+  const unsigned bias_lds = MODE == BIAS ? (unsigned)(uintptr_t)(lds_f32*)bias_row : 0u;
 
   for (int t = t0; t < t1; ++t) {
     const unsigned buf = lds + ((t - t0) & 1) * (2 * TILE);
@@ -72,8 +79,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
     tile_barrier();
     if (t + 1 < t1) {
       const unsigned next = lds + ((t + 1 - t0) & 1) * (2 * TILE);
-      load_tile<T, D, KB, NW>(kb, ks, (t + 1) * KB, len - 1, next, wave, lane);
-      load_tile<T, D, KB, NW>(vb, vs, (t + 1) * KB, len - 1, next + TILE, wave, lane);
+      load_tile<T, D, KB, NW>(kb, ks, (t + 1) * KB, len - 1, next, wave);
+      load_tile<T, D, KB, NW>(vb, vs, (t + 1) * KB, len - 1, next + TILE, wave);
     }
     if (NW > 1 && first_row > last_row) continue;      // (a wave of padding only helps to load)
 #pragma unroll
@@ -87,17 +94,17 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
       const int left = len - key0 - 8 * hi;
 #pragma unroll
       for (int h = 0; h < NQ; ++h) {
-        if constexpr (BIAS) {
+        if constexpr (MODE == BIAS) {
           const int low = key0 - (first_row + 32 * h) - q.q_pos;          // r of key 0 and query 0 of the square
           if (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut) {
             const float far = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
 #pragma unroll
-            for (int a = 0; a < 16; ++a) s[h][a] = __builtin_fmaf(s[h][a], q.c2, far);
+            for (int a = 0; a < 16; ++a) s[h][a] = biased<T>(q, s[h][a], far);
           } else {
             f32x16 bs;
             read_bias<1>(bias_lds + 4 * (low + 8 * hi - (lane & 31) + q.rule.cut + kBiasPad), bs);
 #pragma unroll
-            for (int a = 0; a < 16; ++a) s[h][a] = __builtin_fmaf(s[h][a], q.c2, bs[a]);
+            for (int a = 0; a < 16; ++a) s[h][a] = biased<T>(q, s[h][a], bs[a]);
           }
         }
         if (key0 + 32 > len) {
@@ -108,7 +115,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
 #pragma unroll
         for (int a = 1; a < 16; ++a) m = fmaxf(m, s[h][a]);
         m = max_across_halves(m);
-        mx[h] = BIAS ? m : m * q.c2;
+        mx[h] = MODE == BIAS ? m : m * q.c2;
         moves = moves || mx[h] - ref[h] > kLazy;
       }
       if (__any(moves)) {
@@ -127,7 +134,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
       for (int h = 0; h < NQ; ++h) {
 #pragma unroll
         for (int a = 0; a < 16; ++a) {
-          s[h][a] = exp2_fast(BIAS ? s[h][a] - ref[h] : __builtin_fmaf(s[h][a], q.c2, -ref[h]));
+          s[h][a] = MODE == BIAS ? exp2_fast(s[h][a] - ref[h]) : power_of<T>(q, s[h][a], -ref[h]);
           sum[h] += s[h][a];
         }
       }
@@ -147,8 +154,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
     const float l = sum_across_halves(sum[h]);
     if (g.splits == 1) {
       const int rc = min(rr, last_row);
-      store_column<T, D>(g.O + query_offset<BIAS>(q, q.o, b, hd, rc) * (long long)sizeof(T), hi, z[h], l > 0.f ? 1.f / l : 0.f, there);
-      if (g.lse && there && hi == 0) g.lse[bh * g.rows + rr] = l > 0.f ? (ref[h] + __log2f(l)) * kLn2 : -INFINITY;
+      store_column<T, D>(g.O + query_offset<MODE>(q, q.o, b, hd, rc) * (long long)sizeof(T), hi, z[h], l > 0.f ? 1.f / l : 0.f, there);
+      if (g.lse && there && hi == 0) g.lse[bh * g.rows + rr] = log_sum(ref[h], l);
     } else {
       const long long at = item * RT + wave * (32 * NQ) + 32 * h + (lane & 31);
       store_column<float, D>((unsigned char*)(g.part + at * D), hi, z[h], 1.f, there);
@@ -158,11 +165,11 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
 }
 
 // The pieces of a row put together: a wave for each row, in the order of the pieces.
-template <class T, int D, bool BIAS>
+template <class T, int D, int MODE>
 __global__ __launch_bounds__(256) void dense_join_kernel(DenseGeo q, FwdArgs g, int RT) {
   const long long row = (blockIdx.y * (long long)gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  const int heads = BIAS ? q.H : q.Hk;
+  const int heads = heads_of<MODE>(q);
   if (row >= (long long)q.B * heads * g.rows) return;
   const long long bh = row / g.rows;
   const int rr = (int)(row - bh * g.rows), b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads);
@@ -184,32 +191,32 @@ __global__ __launch_bounds__(256) void dense_join_kernel(DenseGeo q, FwdArgs g, 
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(g.part[(first + (long long)s * RT) * D + lane * E + e], f, o[e]);
   }
-  T* out = (T*)g.O + query_offset<BIAS>(q, q.o, b, hd, rr);
+  T* out = (T*)g.O + query_offset<MODE>(q, q.o, b, hd, rr);
 #pragma unroll
   for (int e = 0; e < E; ++e) out[lane * E + e] = (T)(l > 0.f ? o[e] / l : 0.f);
-  if (g.lse && lane == 0) g.lse[row] = l > 0.f ? (top + __log2f(l)) * kLn2 : -INFINITY;
+  if (g.lse && lane == 0) g.lse[row] = log_sum(top, l);
 }
 
 }  // namespace dense
 
 namespace {
 
-template <class T, int D, int NQ, int NW, bool BIAS>
+template <class T, int D, int NQ, int NW, int MODE>
 hipError_t run_fwd(const DenseGeo& q, const FwdPlan& p, dense::FwdArgs a, hipStream_t s) {
-  const size_t lds = BIAS ? dense::bias_entries(q.rule.cut) * sizeof(float) : 0;
-  dense::dense_fwd_kernel<T, D, NQ, NW, BIAS><<<grid_of(a.items), 64 * NW, lds, s>>>(q, a);
+  const size_t lds = MODE == dense::BIAS ? dense::bias_entries(q.rule.cut) * sizeof(float) : 0;
+  dense::dense_fwd_kernel<T, D, NQ, NW, MODE><<<grid_of(a.items), 64 * NW, lds, s>>>(q, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const long long rows = (long long)q.B * dense_heads(q) * a.rows;
-  dense::dense_join_kernel<T, D, BIAS><<<grid_of((rows + 3) / 4), 256, 0, s>>>(q, a, 32 * NQ * NW);
+  dense::dense_join_kernel<T, D, MODE><<<grid_of((rows + 3) / 4), 256, 0, s>>>(q, a, 32 * NQ * NW);
   return hipGetLastError();
 }
 
-template <class T, int D, bool BIAS>
+template <class T, int D, int MODE>
 hipError_t pick_fwd(const DenseGeo& q, const FwdPlan& p, const dense::FwdArgs& a, hipStream_t s) {
-  if (p.waves == 1) return run_fwd<T, D, 1, 1, BIAS>(q, p, a, s);
-  if (p.sets == 1) return run_fwd<T, D, 1, 4, BIAS>(q, p, a, s);
-  if constexpr (sizeof(T) == 2) return run_fwd<T, D, 2, 4, BIAS>(q, p, a, s);
+  if (p.waves == 1) return run_fwd<T, D, 1, 1, MODE>(q, p, a, s);
+  if (p.sets == 1) return run_fwd<T, D, 1, 4, MODE>(q, p, a, s);
+  if constexpr (sizeof(T) == 2) return run_fwd<T, D, 2, 4, MODE>(q, p, a, s);
   return hipErrorInvalidValue;
 }
 
@@ -245,13 +252,16 @@ hipError_t launch_dense_fwd(const DenseGeo& q, const void* Q, const void* K, con
   a.tiles = p.tiles; a.splits = p.splits;
   a.rows = dense_rows(q);
   a.items = (long long)q.B * dense_heads(q) * p.tiles * p.splits;
-  const bool bias = q.bias != 0;
-  if (q.dtype == DA_BF16) {
-    if (q.d == 128) return bias ? pick_fwd<__bf16, 128, true>(q, p, a, s) : pick_fwd<__bf16, 128, false>(q, p, a, s);
-    return bias ? pick_fwd<__bf16, 64, true>(q, p, a, s) : pick_fwd<__bf16, 64, false>(q, p, a, s);
-  }
-  if (q.d == 128) return bias ? pick_fwd<float, 128, true>(q, p, a, s) : pick_fwd<float, 128, false>(q, p, a, s);
-  return bias ? pick_fwd<float, 64, true>(q, p, a, s) : pick_fwd<float, 64, false>(q, p, a, s);
+  auto pick = [&](auto t, auto d) {
+    typedef decltype(t) T;
+    constexpr int D = decltype(d)::value;
+    if (q.bias) return pick_fwd<T, D, dense::BIAS>(q, p, a, s);
+    return dense_packed(q) ? pick_fwd<T, D, dense::PACKED>(q, p, a, s) : pick_fwd<T, D, dense::PLAIN>(q, p, a, s);
+  };
+  const std::integral_constant<int, 64> d64;
+  const std::integral_constant<int, 128> d128;
+  if (q.dtype == DA_BF16) return q.d == 128 ? pick((__bf16)0.f, d128) : pick((__bf16)0.f, d64);
+  return q.d == 128 ? pick(0.f, d128) : pick(0.f, d64);
 }
 
 }  // namespace da

@@ -326,8 +326,49 @@ __device__ __forceinline__ long long xcd_order(long long id, long long total) {
   return x * each + min(x, more) + id / 8;
 }
 
-// rows of a tile: 16 KB of K and of V at most, so that two workgroups of two buffers fit a CU
-template <class T, int D> constexpr int kKeys = kRowBytes<T, D> > 256 ? 32 : 64;
+// Rows of a tile.  Waves that have each 32 or 64 columns of their own share tiles of 16 KB at most, so that two workgroups of two pairs of
+// buffers fit a CU.  Where there are too few columns for that, JW waves have the same 32 columns and take the 32 rows of JW in turn
+// (their sums are put together at the end, join_waves): tiles of 32 JW rows.
+template <class T, int D, int JW> constexpr int kTileRows = JW > 1 ? 32 * JW : kRowBytes<T, D> > 256 ? 32 : 64;
+// the most waves that may join: tiles of K and V, twice, in 128 KB
+template <class T, int D> constexpr int kJoin = kRowBytes<T, D> > 256 ? 2 : 4;
+
+// Z of JW waves over the same 32 columns, each times its wave's f, added up in the order of the waves; `put(row, channel, x)` gets 8 channels
+// of a row at a time.  The tiles' memory is free by then (every wave behind the first barrier).
+template <int D, int JW, class Put>
+__device__ __forceinline__ void join_waves(float* buf, int wave, int lane, const f32x16 (&z)[D / 32], float f, Put put) {
+  constexpr int S = D + 4;         // row stride: 16 lanes' pieces in 64 banks
+  tile_barrier();
+  float* mine = buf + (wave * 32 + (lane & 31)) * S + 4 * (lane >> 5);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) *(f32x4*)(mine + 32 * dt + 8 * k) = f32x4{z[dt][4 * k] * f, z[dt][4 * k + 1] * f, z[dt][4 * k + 2] * f, z[dt][4 * k + 3] * f};
+  tile_barrier();
+  for (int i = wave * 64 + lane; i < 32 * (D / 8); i += 64 * JW) {
+    const int row = i / (D / 8), c = i % (D / 8) * 8;
+    f32x4 x[2] = {};
+#pragma unroll
+    for (int w = 0; w < JW; ++w) {
+      x[0] += *(const f32x4*)(buf + (w * 32 + row) * S + c);
+      x[1] += *(const f32x4*)(buf + (w * 32 + row) * S + c + 4);
+    }
+    put(row, c, x);
+  }
+}
+
+// 8 channels to their place in the result's type
+template <class T> __device__ __forceinline__ void store8(unsigned char* at, const f32x4 (&x)[2], float f) {
+  if constexpr (sizeof(T) == 2) {
+    bf16x8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (__bf16)(x[i >> 2][i & 3] * f);
+    *(bf16x8*)at = y;
+  } else {
+    *(f32x4*)at = x[0] * f;
+    *(f32x4*)(at + 16) = x[1] * f;
+  }
+}
 
 // What a launch is made for: its queries' rows are those of single heads, the same with a bias, or those of several heads (dense_packed).
 enum Mode { PLAIN, BIAS, PACKED };
@@ -353,9 +394,25 @@ template <class T> __device__ __forceinline__ float power_of(const DenseGeo& q, 
 
 constexpr int kCUs = 256;
 
-inline dim3 grid_of(long long n) {            // n workgroups of at most 256 threads, in as many rows as the limit of 2^32 threads along x makes
+inline dim3 grid_of(long long n) {     // n workgroups of at most 256 threads, in as many rows as the limit of 2^32 threads along x makes
   const long long x = n < (1LL << 23) ? n : (1LL << 23);
   return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
 }
+
+// Into how many pieces each of `wgs` workgroups is cut that go through `units` tiles (unit_us each, with two workgroups to a CU), where the
+// sums of the pieces have to be written and read again (join_mb, for each piece).  A launch takes whole rounds of `slots` workgroups, so the
+// rounds times a piece's tiles (and one for its beginning and end) are weighed against the join, at 4 TB/s and 6 us for its launch.
+inline int cut(long long wgs, long long units, int slots, double unit_us, double join_mb) {
+  int best = 1;
+  double least = 0;
+  for (int n = 1; n <= 64 && (n == 1 || units / n >= 4); ++n) {
+    const double rounds = (double)((wgs * n + slots - 1) / slots);
+    const double us = rounds * (double)((units + n - 1) / n + 1) * unit_us + (n > 1 ? 6.0 + 0.5 * n * join_mb : 0.0);
+    if (n == 1 || us < least) least = us, best = n;
+  }
+  return best;
+}
+// us of a tile for one product, two workgroups of four waves to a CU: bf16 64 rows, float32 64 rows of 64 or 32 of 128 channels
+inline double product_us(const DenseGeo& q) { return q.dtype == DA_F32 ? 3.4 : q.d == 128 ? 0.85 : 0.5; }
 
 }  // namespace da

@@ -24,10 +24,10 @@ inline bool dense_packed(const DenseGeo& q) { return !q.bias && q.group > 1 && q
 inline int dense_heads(const DenseGeo& q) { return dense_packed(q) ? q.Hk : q.H; }
 inline long long dense_rows(const DenseGeo& q) { return dense_packed(q) ? (long long)q.group * q.N : q.N; }
 
-// How the work is cut (host rule; the reasons stand at the functions)
+// How the work of the forward pass is cut (host rule; the reasons stand at the function)
 struct FwdPlan {
-  int waves, sets;       // waves of a workgroup, sets of 32 queries of a wave
-  int tiles, splits;     // tiles of queries of a head, pieces of the keys
+  int join, sets;        // waves share their queries; else sets of 32 queries of a wave
+  int row_tile, tiles, splits;   // queries of a workgroup, tiles of them of a head, pieces of the keys
 };
 FwdPlan plan_dense_fwd(const DenseGeo& q);
 size_t dense_fwd_workspace(const DenseGeo& q);

@@ -68,11 +68,11 @@ __device__ __forceinline__ void bucket_range(const RelRule& t, int c, int& first
 // Minus infinity where a row has nothing to attend or is padding: p is 0.
 template <class T> __device__ __forceinline__ float start_of(const DenseGeo& q, float lse2) { return sizeof(T) == 2 ? -lse2 / q.c2 : -lse2; }
 
-template <class T, int D, int NW> constexpr int kDqWaves = NW == 1 || kRowBytes<T, D> > 256 ? 1 : 2;
+template <class T, int D, int JW> constexpr int kDqWaves = JW > 1 || kRowBytes<T, D> > 256 ? 1 : 2;
 
-template <class T, int D, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, NW>)) void dense_dq_kernel(DenseGeo q, BwdArgs g) {
-  constexpr int KB = kKeys<T, D>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * NW;
+template <class T, int D, int NW, int JW, int MODE>
+__global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel(DenseGeo q, BwdArgs g) {
+  constexpr int KB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * (NW / JW);
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * TILE];
   extern __shared__ __attribute__((aligned(16))) float bias_row[];
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, NW>)) void dense_dq_kernel
   const int heads = heads_of<MODE>(q);
   const int b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads), hk = kv_head<MODE>(q, hd);
   const int len = q.kv_len ? min(max(q.kv_len[b], 0), q.M) : q.M;
-  const int first_row = tile * RT + wave * 32, last_row = (int)g.rows - 1;
+  const int first_row = tile * RT + (JW > 1 ? 0 : wave * 32), last_row = (int)g.rows - 1;
   const int n_tiles = (len + KB - 1) / KB, each = (n_tiles + g.splits - 1) / g.splits;
   const int t0 = min(split * each, n_tiles), t1 = min(t0 + each, n_tiles);
   const long long ks = q.k.sn * (long long)sizeof(T), vs = q.v.sn * (long long)sizeof(T);
@@ -129,9 +129,10 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, NW>)) void dense_dq_kernel
       load_tile<T, D, KB, NW>(kb, ks, (t + 1) * KB, len - 1, next, wave);
       load_tile<T, D, KB, NW>(vb, vs, (t + 1) * KB, len - 1, next + TILE, wave);
     }
-    if (NW > 1 && first_row > last_row) continue;
+    if (first_row > last_row) continue;
 #pragma unroll
-    for (int sub = 0; sub < KB / 32; ++sub) {
+    for (int i = 0; i < KB / 32 / JW; ++i) {
+      const int sub = JW > 1 ? wave : i;
       const int key0 = t * KB + 32 * sub;
       if (key0 >= len) break;
       f32x16 s[1], dp[1];
@@ -169,7 +170,22 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, NW>)) void dense_dq_kernel
   }
   off = sum_across_halves(off);
   const bool there = rr <= last_row;
-  if (g.splits == 1) {
+  if constexpr (JW > 1) {
+    float* buf = (float*)tiles;
+    float* sums = buf + NW * 32 * (D + 4);
+    join_waves<D, NW>(buf, wave, lane, z[0], q.scale, [&](int row, int c, f32x4 (&x)[2]) {
+      if (first_row + row > last_row) return;
+      if (g.splits == 1) store8<T>(g.dQ + (query_offset<MODE>(q, q.dq, b, hd, first_row + row) + c) * (long long)sizeof(T), x, 1.f);
+      else store8<float>((unsigned char*)(g.dq_part + (item * RT + row) * D + c), x, 1.f);
+    });
+    if (hi == 0) sums[wave * 32 + lane] = off;
+    __syncthreads();
+    off = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) off += sums[w * 32 + (lane & 31)];
+    if (wave != 0) return;
+    if (g.splits > 1 && there && hi == 0) g.r_part[item * RT + lane] = off;
+  } else if (g.splits == 1) {
     store_column<T, D>(g.dQ + query_offset<MODE>(q, q.dq, b, hd, rc) * (long long)sizeof(T), hi, z[0], q.scale, there);
   } else {
     const long long at = item * RT + wave * 32 + (lane & 31);
@@ -183,11 +199,11 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, NW>)) void dense_dq_kernel
 }
 
 // waves to a SIMD that the kernel below is made for
-template <class T, int D, int NK, int NW> constexpr int kDkvWaves = NW == 1 || NK == 2 || kRowBytes<T, D> > 256 ? 1 : 2;
+template <class T, int D, int JW> constexpr int kDkvWaves = JW > 1 || kRowBytes<T, D> > 256 ? 1 : 2;
 
-template <class T, int D, int NK, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, NK, NW>)) void dense_dkv_kernel(DenseGeo q, BwdArgs g) {
-  constexpr int QB = kKeys<T, D>, RB = kRowBytes<T, D>, TILE = QB * RB, STAGE = 2 * TILE + 1024, KT = 32 * NK * NW;
+template <class T, int D, int NW, int JW, int MODE>
+__global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kernel(DenseGeo q, BwdArgs g) {
+  constexpr int QB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>, TILE = QB * RB, STAGE = 2 * TILE + 1024, KT = 32 * (NW / JW);
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[2 * STAGE];  // twice: Q, dO, lse2 and delta of their rows
   extern __shared__ __attribute__((aligned(16))) float bias_row[];           // then per wave its diagonals and its square
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
@@ -201,7 +217,7 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, NK, NW>)) void dense_dkv_
   const long long bh = rest / g.splits;
   const int b = (int)(bh / q.Hk), hk = (int)(bh - (long long)b * q.Hk);
   const int len = q.kv_len ? min(max(q.kv_len[b], 0), q.M) : q.M;
-  const int key0 = tile * KT + wave * (32 * NK);
+  const int key0 = tile * KT + (JW > 1 ? 0 : wave * 32);
   const int hd = MODE == PACKED || q.group == 1 ? hk : hk * q.group + split / g.per_head;
   const int piece = MODE == PACKED || q.group == 1 ? split : split % g.per_head;
   const long long stat = ((long long)b * heads_of<MODE>(q) + hd) * g.padded;
@@ -228,9 +244,13 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, NK, NW>)) void dense_dkv_
         dma16(g.dO + query_offset<MODE>(q, q.dout, b, hd, rr) * (long long)sizeof(T) + p, to + TILE + it * 1024);
       }
     }
-    const long long rr = stat + min((long long)first + lane, g.padded - 1);
-    if (wave == 0) dma4(g.start + rr, to + 2 * TILE);
-    if (wave == (NW > 1 ? 1 : 0)) dma4(g.delta + rr, to + 2 * TILE + 256);
+    constexpr int CH = QB > 64 ? QB / 64 : 1;        // 64 rows' numbers at a time
+#pragma unroll
+    for (int i = 0; i < 2 * CH; ++i) {
+      if (i % NW != wave) continue;
+      const long long rr = stat + min((long long)first + 64 * (i % CH) + lane, g.padded - 1);
+      dma4((i / CH ? g.delta : g.start) + rr, to + 2 * TILE + 512 * (i / CH) + 256 * (i % CH));
+    }
   };
   if (t0 < t1) load_rows(t0, lds);
   const int n_bias = MODE == BIAS ? (bias_entries(q.rule.cut) + 3) & ~3 : 0;
@@ -241,17 +261,14 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, NK, NW>)) void dense_dkv_
     for (int i = lane; i < n_bias; i += 64) diag[i] = 0.f;
   }
 
-  Own<T, D> own_k[NK], own_v[NK];
-  f32x16 zk[NK][D / 32], zv[NK][D / 32];
+  Own<T, D> own_k[1], own_v[1];
+  f32x16 zk[1][D / 32], zv[1][D / 32];
 #pragma unroll
-  for (int h = 0; h < NK; ++h) {
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) zk[h][dt] = zv[h][dt] = zero16();
-    if (t0 < t1) {
-      const long long kc = min(key0 + 32 * h + (lane & 31), len - 1);
-      own_k[h].load(g.K + (b * q.k.sb + hk * q.k.sh + kc * q.k.sn) * (long long)sizeof(T), hi);
-      own_v[h].load(g.V + (b * q.v.sb + hk * q.v.sh + kc * q.v.sn) * (long long)sizeof(T), hi);
-    }
+  for (int dt = 0; dt < D / 32; ++dt) zk[0][dt] = zv[0][dt] = zero16();
+  if (t0 < t1) {
+    const long long kc = min(key0 + (lane & 31), len - 1);
+    own_k[0].load(g.K + (b * q.k.sb + hk * q.k.sh + kc * q.k.sn) * (long long)sizeof(T), hi);
+    own_v[0].load(g.V + (b * q.v.sb + hk * q.v.sh + kc * q.v.sn) * (long long)sizeof(T), hi);
   }
   const unsigned s_lane = scores_lane<T, D>(lane), m_lane = mix_lane<T, D>(lane);
   const unsigned bias_lds = MODE == BIAS ? (unsigned)(uintptr_t)(lds_f32*)bias_row : 0u;
@@ -261,110 +278,117 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, NK, NW>)) void dense_dkv_
     wait_loads();
     tile_barrier();
     if (t + 1 < t1) load_rows(t + 1, lds + ((t + 1 - t0) & 1) * STAGE);
-    if (NW > 1 && key0 >= len) continue;
+    if (key0 >= len) continue;
 #pragma unroll
-    for (int sub = 0; sub < QB / 32; ++sub) {
+    for (int i = 0; i < QB / 32 / JW; ++i) {
+      const int sub = JW > 1 ? wave : i;
       const int row0 = t * QB + 32 * sub;
       if (row0 > last_row) break;
       // Sums start from what belongs to their rows (start_of, -delta): registers 4i .. 4i + 3 have rows 16(i / 2) + 8 hi + 4(i % 2) + 0..3.
       constexpr bool kLate = sizeof(T) == 4;
-      f32x16 s[NK], dp[NK], late;
+      f32x16 s[1], dp[1], late;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const unsigned at = buf + 2 * TILE + 4 * (32 * sub + 16 * (i >> 1) + 8 * hi + 4 * (i & 1));
-        const f32x4 l = *(lds_f32x4*)(uintptr_t)at, dl = *(lds_f32x4*)(uintptr_t)(at + 256);
+        const f32x4 l = *(lds_f32x4*)(uintptr_t)at, dl = *(lds_f32x4*)(uintptr_t)(at + 512);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           late[4 * i + e] = kLate ? l[e] : 0.f;
-#pragma unroll
-          for (int h = 0; h < NK; ++h) {
-            s[h][4 * i + e] = kLate ? 0.f : l[e];
-            dp[h][4 * i + e] = dl[e];
-          }
+          s[0][4 * i + e] = kLate ? 0.f : l[e];
+          dp[0][4 * i + e] = dl[e];
         }
       }
-      add_scores<T, D, NK>(buf + sub * 32 * RB + s_lane, own_k, s);
-      add_scores<T, D, NK>(buf + TILE + sub * 32 * RB + s_lane, own_v, dp);
-      Mixed<T> p[NK], ds[NK];
+      add_scores<T, D, 1>(buf + sub * 32 * RB + s_lane, own_k, s);
+      add_scores<T, D, 1>(buf + TILE + sub * 32 * RB + s_lane, own_v, dp);
+      const int low = MODE == BIAS ? key0 - row0 - q.q_pos : 0;      // r of key 0 and query 0 of the square
+      const bool is_far = MODE == BIAS && (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut);
+      if constexpr (MODE == BIAS) {
+        if (is_far) {
+          const float far = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
 #pragma unroll
-      for (int h = 0; h < NK; ++h) {
-        const int low = MODE == BIAS ? key0 + 32 * h - row0 - q.q_pos : 0;      // r of key 0 and query 0 of the square
-        const bool is_far = MODE == BIAS && (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut);
-        if constexpr (MODE == BIAS) {
-          if (is_far) {
-            const float far = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
-#pragma unroll
-            for (int a = 0; a < 16; ++a) s[h][a] = power_of<T>(q, s[h][a], kLate ? far + late[a] : far);
-          } else {
-            f32x16 bs;
-            read_bias<-1>(bias_lds + 4 * (low + (lane & 31) - 8 * hi + q.rule.cut + kBiasPad), bs);
-#pragma unroll
-            for (int a = 0; a < 16; ++a) s[h][a] = power_of<T>(q, s[h][a], kLate ? bs[a] + late[a] : bs[a]);
-          }
+          for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], kLate ? far + late[a] : far);
         } else {
+          f32x16 bs;
+          read_bias<-1>(bias_lds + 4 * (low + (lane & 31) - 8 * hi + q.rule.cut + kBiasPad), bs);
 #pragma unroll
-          for (int a = 0; a < 16; ++a) s[h][a] = kLate ? power_of<T>(q, s[h][a], late[a]) : exp2_fast(s[h][a] * q.c2);
+          for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], kLate ? bs[a] + late[a] : bs[a]);
         }
-        p[h] = Mixed<T>(s[h]);
+      } else {
 #pragma unroll
-        for (int a = 0; a < 16; ++a) dp[h][a] *= s[h][a];
-        ds[h] = Mixed<T>(dp[h]);
-        if constexpr (MODE == BIAS) {
-          if (key0 + 32 * h + 32 > len) {
-            const bool is_there = key0 + 32 * h + (lane & 31) < len;
+        for (int a = 0; a < 16; ++a) s[0][a] = kLate ? power_of<T>(q, s[0][a], late[a]) : exp2_fast(s[0][a] * q.c2);
+      }
+      const Mixed<T> p[1] = {Mixed<T>(s[0])};
 #pragma unroll
-            for (int a = 0; a < 16; ++a) dp[h][a] = is_there ? dp[h][a] : 0.f;
+      for (int a = 0; a < 16; ++a) dp[0][a] *= s[0][a];
+      const Mixed<T> ds[1] = {Mixed<T>(dp[0])};
+      if constexpr (MODE == BIAS) {
+        if (key0 + 32 > len) {
+          const bool is_there = key0 + (lane & 31) < len;
+#pragma unroll
+          for (int a = 0; a < 16; ++a) dp[0][a] = is_there ? dp[0][a] : 0.f;
+        }
+        if (is_far) {
+          float x = 0.f;
+#pragma unroll
+          for (int a = 0; a < 16; ++a) x += dp[0][a];
+          far_sum[0] += low > 0 ? 0.f : x;
+          far_sum[1] += low > 0 ? x : 0.f;
+        } else {
+          // Diagonals of the square (key n, query m; r = low + n - m): by way of LDS lane c reads the queries (n - c) mod 32 of half the
+          // keys, whose sum belongs to r = low + c where n >= c and to low + c - 32 elsewhere.
+          f32x4* row = (f32x4*)(square + (lane & 31) * kScratch + 8 * hi);
+          row[0] = f32x4{dp[0][0], dp[0][1], dp[0][2], dp[0][3]};
+          row[1] = f32x4{dp[0][4], dp[0][5], dp[0][6], dp[0][7]};
+          row[4] = f32x4{dp[0][8], dp[0][9], dp[0][10], dp[0][11]};
+          row[5] = f32x4{dp[0][12], dp[0][13], dp[0][14], dp[0][15]};
+          __builtin_amdgcn_wave_barrier();
+          const int c = lane & 31;
+          float straight = 0.f, wrapped = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int n = 2 * i + hi;
+            const float x = square[n * kScratch + ((n - c) & 31)];
+            straight += n >= c ? x : 0.f;
+            wrapped += n >= c ? 0.f : x;
           }
-          if (is_far) {
-            float x = 0.f;
-#pragma unroll
-            for (int a = 0; a < 16; ++a) x += dp[h][a];
-            far_sum[0] += low > 0 ? 0.f : x;
-            far_sum[1] += low > 0 ? x : 0.f;
-          } else {
-            // Diagonals of the square (key n, query m; r = low + n - m): by way of LDS lane c reads the queries (n - c) mod 32 of half the
-            // keys, whose sum belongs to r = low + c where n >= c and to low + c - 32 elsewhere.
-            f32x4* row = (f32x4*)(square + (lane & 31) * kScratch + 8 * hi);
-            row[0] = f32x4{dp[h][0], dp[h][1], dp[h][2], dp[h][3]};
-            row[1] = f32x4{dp[h][4], dp[h][5], dp[h][6], dp[h][7]};
-            row[4] = f32x4{dp[h][8], dp[h][9], dp[h][10], dp[h][11]};
-            row[5] = f32x4{dp[h][12], dp[h][13], dp[h][14], dp[h][15]};
-            __builtin_amdgcn_wave_barrier();
-            const int c = lane & 31;
-            float straight = 0.f, wrapped = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int n = 2 * i + hi;
-              const float x = square[n * kScratch + ((n - c) & 31)];
-              straight += n >= c ? x : 0.f;
-              wrapped += n >= c ? 0.f : x;
-            }
-            const float d0 = sum_across_halves(straight), d1 = sum_across_halves(wrapped);
-            diag[low + (hi ? c - 32 : c) + q.rule.cut + kBiasPad] += hi ? d1 : d0;
-            __builtin_amdgcn_wave_barrier();
-          }
+          const float d0 = sum_across_halves(straight), d1 = sum_across_halves(wrapped);
+          diag[low + (hi ? c - 32 : c) + q.rule.cut + kBiasPad] += hi ? d1 : d0;
+          __builtin_amdgcn_wave_barrier();
         }
       }
-      mix<T, D, NK>(buf + TILE + sub * 32 * RB + m_lane, p, zv);
-      mix<T, D, NK>(buf + sub * 32 * RB + m_lane, ds, zk);
+      mix<T, D, 1>(buf + TILE + sub * 32 * RB + m_lane, p, zv);
+      mix<T, D, 1>(buf + sub * 32 * RB + m_lane, ds, zk);
     }
   }
-#pragma unroll
-  for (int h = 0; h < NK; ++h) {
-    const int key = key0 + 32 * h + (lane & 31);
+  const long long bhs = (long long)q.B * q.Hk;
+  float* part = g.dkv_part + (split * bhs + bh) * q.M * D;               // K's, and V's behind all of K's
+  const long long v_part = g.splits * bhs * q.M * D;
+  unsigned char* dk = g.dK + (b * q.dk.sb + hk * q.dk.sh) * (long long)sizeof(T);
+  unsigned char* dv = g.dV + (b * q.dv.sb + hk * q.dv.sh) * (long long)sizeof(T);
+  if constexpr (JW > 1) {
+    auto put = [&](unsigned char* out, long long stride, float* parts, int row, int c, f32x4 (&x)[2]) {
+      const int key = key0 + row;
+      if (key >= len) x[0] = x[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (g.splits > 1 ? key >= len : key >= q.M) return;
+      if (g.splits > 1) store8<float>((unsigned char*)(parts + (long long)key * D + c), x, 1.f);
+      else store8<T>(out + (key * stride + c) * (long long)sizeof(T), x, 1.f);
+    };
+    float* buf = (float*)tiles;
+    join_waves<D, NW>(buf, wave, lane, zk[0], q.scale, [&](int row, int c, f32x4 (&x)[2]) { put(dk, q.dk.sn, part, row, c, x); });
+    join_waves<D, NW>(buf, wave, lane, zv[0], 1.f, [&](int row, int c, f32x4 (&x)[2]) { put(dv, q.dv.sn, part + v_part, row, c, x); });
+  } else {
+    const int key = key0 + (lane & 31);
     const long long kc = min(key, q.M - 1);
     if (g.splits == 1) {
       if (key >= len) {
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) zk[h][dt] = zv[h][dt] = zero16();
+        for (int dt = 0; dt < D / 32; ++dt) zk[0][dt] = zv[0][dt] = zero16();
       }
-      store_column<T, D>(g.dK + (b * q.dk.sb + hk * q.dk.sh + kc * q.dk.sn) * (long long)sizeof(T), hi, zk[h], q.scale, key < q.M);
-      store_column<T, D>(g.dV + (b * q.dv.sb + hk * q.dv.sh + kc * q.dv.sn) * (long long)sizeof(T), hi, zv[h], 1.f, key < q.M);
+      store_column<T, D>(dk + kc * q.dk.sn * (long long)sizeof(T), hi, zk[0], q.scale, key < q.M);
+      store_column<T, D>(dv + kc * q.dv.sn * (long long)sizeof(T), hi, zv[0], 1.f, key < q.M);
     } else {
-      const long long bhs = (long long)q.B * q.Hk;
-      float* at = g.dkv_part + ((split * bhs + bh) * q.M + kc) * D;
-      store_column<float, D>((unsigned char*)at, hi, zk[h], q.scale, key < len);
-      store_column<float, D>((unsigned char*)(at + g.splits * bhs * q.M * D), hi, zv[h], 1.f, key < len);
+      store_column<float, D>((unsigned char*)(part + kc * D), hi, zk[0], q.scale, key < len);
+      store_column<float, D>((unsigned char*)(part + v_part + kc * D), hi, zv[0], 1.f, key < len);
     }
   }
   if constexpr (MODE == BIAS) {
@@ -466,68 +490,86 @@ __global__ __launch_bounds__(256) void dense_sum_bias_kernel(DenseGeo q, BwdArgs
 
 namespace {
 
+constexpr size_t kLds = 160 * 1024;
+
 struct BwdPlan {
-  int waves, tiles, splits;                          // dq
-  int kv_waves, kv_sets, kv_tiles, kv_splits, per_head, row_tiles;  // dkv
+  int join, row_tile, tiles, splits;                                            // dq
+  int kv_join, kv_tiles, kv_splits, per_head, row_tiles, q_tile;                // dkv
   size_t start, delta, dq_part, r_part, dkv_part, bias_part, total;
 };
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// sets of 32 keys of a wave
-constexpr int dkv_sets(bool bf16, int d, int waves) { return bf16 && d == 64 && waves == 4 ? 2 : 1; }
+// LDS of the second kernel beside its tiles: bias, diagonals and squares of `waves` waves
+inline size_t dkv_bias_lds(const DenseGeo& q, int waves) {
+  if (!q.bias) return 0;
+  const size_t n = (dense::bias_entries(q.rule.cut) + 3) & ~3;
+  return (n + waves * (n + 32 * dense::kScratch)) * sizeof(float);
+}
 
+// Workgroups of four waves with 32 queries (keys) each, or, where they are too few, of waves that share 32 and take the other side in turn.
 BwdPlan plan_bwd(const DenseGeo& q) {
   BwdPlan p;
   const long long rows = dense_rows(q), heads = (long long)q.B * dense_heads(q), kv_heads = (long long)q.B * q.Hk;
-  const int tile = q.dtype == DA_F32 && q.d == 128 ? 32 : 64;
-  p.waves = rows <= 64 ? 1 : 4;
-  const int rt = 32 * p.waves;
-  p.tiles = (int)((rows + rt - 1) / rt);
-  const long long want = 2 * kCUs, key_tiles = (q.M + tile - 1) / tile;
-  auto pieces = [&](long long wgs, long long units) {
-    long long n = wgs >= want ? 1 : (want + wgs - 1) / wgs;
-    n = n > units / 4 ? units / 4 : n;
+  const bool f32 = q.dtype == DA_F32;
+  const int row_bytes = q.d * (f32 ? 4 : 2), tile = row_bytes > 256 ? 32 : 64, enough = kCUs / 4 * 3;
+  const int joined = row_bytes > 256 ? 64 : 128, join_slots = row_bytes == 128 ? 2 * kCUs : kCUs;      // rows of a joining workgroup's tile
+  const int slots = row_bytes > 256 ? kCUs : 2 * kCUs;                                                 // (one wave to a SIMD there)
+  auto pieces_joined = [&](long long wgs, long long units) {
+    long long n = join_slots / wgs;
+    n = n > units / 2 ? units / 2 : n;
     return (int)(n < 1 ? 1 : n);
   };
-  p.splits = pieces(heads * p.tiles, key_tiles);
-  p.kv_waves = q.M <= 32 ? 1 : 4;
-  p.kv_sets = dkv_sets(q.dtype == DA_BF16, q.d, p.kv_waves);
-  const int kt = 32 * p.kv_sets * p.kv_waves;
-  p.kv_tiles = (q.M + kt - 1) / kt;
-  p.row_tiles = (int)((rows + tile - 1) / tile);
+  long long wgs = heads * ((rows + 127) / 128);
+  p.join = 0;
+  p.splits = rows > 64 ? cut(wgs, (q.M + tile - 1) / tile, slots, 3 * product_us(q), 128.0 * wgs * q.d * 4e-6) : 1;
+  if (wgs * p.splits < enough) {
+    p.join = 1;
+    p.splits = pieces_joined(heads * ((rows + 31) / 32), (q.M + joined - 1) / joined);
+  }
+  p.row_tile = p.join ? 32 : 128;
+  p.tiles = (int)((rows + p.row_tile - 1) / p.row_tile);
   const int stretches = dense_packed(q) ? 1 : q.group;   // a piece stays within the rows of a head
-  p.per_head = pieces(kv_heads * p.kv_tiles * stretches, p.row_tiles);
+  wgs = kv_heads * stretches * ((q.M + 127) / 128);
+  p.kv_join = 0;
+  p.per_head = q.M > 64 ? cut(wgs, (rows + tile - 1) / tile, slots, 4 * product_us(q), 2.0 * kv_heads * q.M * q.d * 4e-6) : 1;
+  const size_t tiles_lds = 2 * (2 * (size_t)joined * row_bytes + 1024);
+  if (wgs * p.per_head < enough && tiles_lds + dkv_bias_lds(q, row_bytes > 256 ? 2 : 4) <= kLds) {
+    p.kv_join = 1;
+    p.per_head = pieces_joined(kv_heads * stretches * ((q.M + 31) / 32), (rows + joined - 1) / joined);
+  }
+  const int kt = p.kv_join ? 32 : 128;
+  p.q_tile = p.kv_join ? joined : tile;
+  p.kv_tiles = (q.M + kt - 1) / kt;
+  p.row_tiles = (int)((rows + p.q_tile - 1) / p.q_tile);
   p.kv_splits = p.per_head * stretches;
   const size_t padded = (size_t)(rows + 31) / 32 * 32;
   size_t off = 0;
   p.start = off; off += align_up(heads * padded * sizeof(float));
   p.delta = off; off += align_up(heads * padded * sizeof(float));
-  p.dq_part = off; off += p.splits > 1 ? align_up((size_t)heads * p.tiles * p.splits * rt * q.d * sizeof(float)) : 0;
-  p.r_part = off; off += p.splits > 1 ? align_up((size_t)heads * p.tiles * p.splits * rt * sizeof(float)) : 0;
+  p.dq_part = off; off += p.splits > 1 ? align_up((size_t)heads * p.tiles * p.splits * p.row_tile * q.d * sizeof(float)) : 0;
+  p.r_part = off; off += p.splits > 1 ? align_up((size_t)heads * p.tiles * p.splits * p.row_tile * sizeof(float)) : 0;
   p.dkv_part = off; off += p.kv_splits > 1 ? align_up(2 * (size_t)p.kv_splits * kv_heads * q.M * q.d * sizeof(float)) : 0;
   p.bias_part = off; off += q.bias ? align_up((size_t)kv_heads * p.kv_tiles * p.kv_splits * q.buckets * sizeof(float)) : 0;
   p.total = off;
   return p;
 }
 
-template <class T, int D, int NW, int MODE>
+template <class T, int D, int NW, int JW, int MODE>
 hipError_t run_dq(const DenseGeo& q, const BwdPlan& p, const dense::BwdArgs& a, hipStream_t s) {
   const size_t lds = MODE == dense::BIAS ? dense::bias_entries(q.rule.cut) * sizeof(float) : 0;
-  dense::dense_dq_kernel<T, D, NW, MODE><<<grid_of(a.items), 64 * NW, lds, s>>>(q, a);
+  dense::dense_dq_kernel<T, D, NW, JW, MODE><<<grid_of(a.items), 64 * NW, lds, s>>>(q, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const long long rows = (long long)q.B * dense_heads(q) * a.rows;
   constexpr int R = 256 / (D / 4);
-  dense::dense_sum_dq_kernel<T, D, MODE><<<grid_of((rows + R - 1) / R), 256, 0, s>>>(q, a, 32 * NW);
+  dense::dense_sum_dq_kernel<T, D, MODE><<<grid_of((rows + R - 1) / R), 256, 0, s>>>(q, a, 32 * (NW / JW));
   return hipGetLastError();
 }
 
-template <class T, int D, int NW, int MODE>
+template <class T, int D, int NW, int JW, int MODE>
 hipError_t run_dkv(const DenseGeo& q, const BwdPlan& p, const dense::BwdArgs& a, hipStream_t s) {
-  const size_t n = (dense::bias_entries(q.rule.cut) + 3) & ~3;
-  const size_t lds = MODE == dense::BIAS ? (n + NW * (n + 32 * dense::kScratch)) * sizeof(float) : 0;
-  dense::dense_dkv_kernel<T, D, dkv_sets(sizeof(T) == 2, D, NW), NW, MODE><<<grid_of(a.items), 64 * NW, lds, s>>>(q, a);
+  dense::dense_dkv_kernel<T, D, NW, JW, MODE><<<grid_of(a.items), 64 * NW, dkv_bias_lds(q, NW), s>>>(q, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (MODE == dense::BIAS) {
@@ -542,13 +584,14 @@ hipError_t run_dkv(const DenseGeo& q, const BwdPlan& p, const dense::BwdArgs& a,
 
 template <class T, int D, int MODE>
 hipError_t run_bwd(const DenseGeo& q, const BwdPlan& p, dense::BwdArgs a, hipStream_t s) {
+  constexpr int J = dense::kJoin<T, D>;
   a.tiles = p.tiles; a.splits = p.splits;
   a.items = (long long)q.B * dense_heads(q) * p.tiles * p.splits;
-  hipError_t e = p.waves == 1 ? run_dq<T, D, 1, MODE>(q, p, a, s) : run_dq<T, D, 4, MODE>(q, p, a, s);
+  hipError_t e = p.join ? run_dq<T, D, J, J, MODE>(q, p, a, s) : run_dq<T, D, 4, 1, MODE>(q, p, a, s);
   if (e != hipSuccess) return e;
   a.tiles = p.kv_tiles; a.splits = p.kv_splits; a.per_head = p.per_head; a.row_tiles = p.row_tiles;
   a.items = (long long)q.B * q.Hk * p.kv_tiles * p.kv_splits;
-  return p.kv_waves == 1 ? run_dkv<T, D, 1, MODE>(q, p, a, s) : run_dkv<T, D, 4, MODE>(q, p, a, s);
+  return p.kv_join ? run_dkv<T, D, J, J, MODE>(q, p, a, s) : run_dkv<T, D, 4, 1, MODE>(q, p, a, s);
 }
 
 }  // namespace

@@ -27,9 +27,11 @@ __device__ __forceinline__ float log_sum(float ref, float l) {
   return l > 0.f ? __builtin_fmaf(ref, kLn2, __builtin_fmaf(ref, kLn2Lo, logf(l))) : -INFINITY;
 }
 
-template <class T, int D, int NQ, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(DenseGeo q, FwdArgs g) {
-  constexpr int KB = kKeys<T, D>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * NQ * NW;
+// NW waves, JW of which share their columns (1, or all)
+template <class T, int D, int NQ, int NW, int JW, int MODE>
+__global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(DenseGeo q, FwdArgs g) {
+  static_assert(JW == 1 || (JW == NW && NQ == 1), "one set of columns to join");
+  constexpr int KB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * NQ * (NW / JW);
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * TILE];   // K, V, K, V
   extern __shared__ __attribute__((aligned(16))) float bias_row[];
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
@@ -43,7 +45,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
   const int heads = heads_of<MODE>(q);
   const int b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads), hk = kv_head<MODE>(q, hd);
   const int len = q.kv_len ? min(max(q.kv_len[b], 0), q.M) : q.M;
-  const int first_row = tile * RT + wave * (32 * NQ), last_row = (int)g.rows - 1;
+  const int first_row = tile * RT + (JW > 1 ? 0 : wave * (32 * NQ)), last_row = (int)g.rows - 1;
 
   // this split's keys
   const int n_tiles = (len + KB - 1) / KB, each = (n_tiles + g.splits - 1) / g.splits;
@@ -82,9 +84,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
       load_tile<T, D, KB, NW>(kb, ks, (t + 1) * KB, len - 1, next, wave);
       load_tile<T, D, KB, NW>(vb, vs, (t + 1) * KB, len - 1, next + TILE, wave);
     }
-    if (NW > 1 && first_row > last_row) continue;      // (a wave of padding only helps to load)
+    if (first_row > last_row) continue;                // (a wave of padding only helps to load)
 #pragma unroll
-    for (int sub = 0; sub < KB / 32; ++sub) {
+    for (int i = 0; i < KB / 32 / JW; ++i) {
+      const int sub = JW > 1 ? wave : i;
       const int key0 = t * KB + 32 * sub;
       if (key0 >= len) break;
       f32x16 s[NQ];
@@ -147,6 +150,36 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
       }
     }
   }
+  if constexpr (JW > 1) {
+    // the waves' references and sums, then their sums of P V against the largest reference
+    float* buf = (float*)tiles;
+    f32x2* stat = (f32x2*)(buf + NW * 32 * (D + 4));
+    const float own_sum = sum_across_halves(sum[0]);
+    tile_barrier();
+    if (hi == 0) stat[wave * 32 + lane] = f32x2{ref[0], own_sum};
+    tile_barrier();
+    float top = -FLT_MAX;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, stat[w * 32 + (lane & 31)][0]);
+    join_waves<D, NW>(buf, wave, lane, z[0], exp2_fast(ref[0] - top), [&](int row, int c, f32x4 (&x)[2]) {
+      const int rr = first_row + row;
+      if (rr > last_row) return;
+      float t = -FLT_MAX, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) t = fmaxf(t, stat[w * 32 + row][0]);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) l = __builtin_fmaf(stat[w * 32 + row][1], exp2_fast(stat[w * 32 + row][0] - t), l);
+      if (g.splits == 1) {
+        store8<T>(g.O + (query_offset<MODE>(q, q.o, b, hd, rr) + c) * (long long)sizeof(T), x, l > 0.f ? 1.f / l : 0.f);
+        if (g.lse && c == 0) g.lse[bh * g.rows + rr] = log_sum(t, l);
+      } else {
+        const long long at = item * RT + row;
+        store8<float>((unsigned char*)(g.part + at * D + c), x, 1.f);
+        if (c == 0) *(f32x2*)(g.part + g.items * RT * D + at * 2) = f32x2{t, l};
+      }
+    });
+    return;
+  }
 #pragma unroll
   for (int h = 0; h < NQ; ++h) {
     const int rr = first_row + 32 * h + (lane & 31);
@@ -164,33 +197,54 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void dense_fwd_kernel(Den
   }
 }
 
-// The pieces of a row put together: a wave for each row, in the order of the pieces.
-template <class T, int D, int MODE>
+// The pieces of a row put together, in an order that depends on their number alone: W waves to a row, each with every W-th piece.
+template <class T, int D, int W, int MODE>
 __global__ __launch_bounds__(256) void dense_join_kernel(DenseGeo q, FwdArgs g, int RT) {
-  const long long row = (blockIdx.y * (long long)gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
+  __shared__ float sums[4][D];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, w = wave % W;
+  const long long rows = (long long)q.B * heads_of<MODE>(q) * g.rows;
+  const long long id = (blockIdx.y * (long long)gridDim.x + blockIdx.x) * (4 / W) + wave / W;
+  const long long row = min(id, rows - 1);
   const int heads = heads_of<MODE>(q);
-  if (row >= (long long)q.B * heads * g.rows) return;
   const long long bh = row / g.rows;
   const int rr = (int)(row - bh * g.rows), b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads);
   const int tile = rr / RT;
   const long long first = ((bh * g.tiles + tile) * g.splits) * RT + (rr - tile * RT);
-  const float* stat = g.part + g.items * RT * D;
-  float top = -FLT_MAX;
-  for (int s = 0; s < g.splits; ++s) {
-    const f32x2 x = *(const f32x2*)(stat + (first + (long long)s * RT) * 2);
+  const float* stat = g.part + g.items * RT * D + first * 2;
+  const float* part = g.part + first * D;
+  float top = -FLT_MAX, l = 0.f;
+  for (int s = lane; s < g.splits; s += 64) {
+    const f32x2 x = *(const f32x2*)(stat + (long long)s * RT * 2);
     if (x[1] > 0.f) top = fmaxf(top, x[0]);
   }
-  constexpr int E = D / 64;
-  float o[E] = {}, l = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < g.splits; ++s) {
-    const f32x2 x = *(const f32x2*)(stat + (first + (long long)s * RT) * 2);
-    const float f = x[1] > 0.f ? exp2_fast(x[0] - top) : 0.f;
-    l = __builtin_fmaf(x[1], f, l);
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(g.part[(first + (long long)s * RT) * D + lane * E + e], f, o[e]);
+  for (int i = 32; i >= 1; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+  for (int s = lane; s < g.splits; s += 64) {
+    const f32x2 x = *(const f32x2*)(stat + (long long)s * RT * 2);
+    if (x[1] > 0.f) l = __builtin_fmaf(x[1], exp2_fast(x[0] - top), l);
   }
+#pragma unroll
+  for (int i = 32; i >= 1; i >>= 1) l += __shfl_xor(l, i);
+  constexpr int E = D / 64;
+  float o[E] = {};
+#pragma unroll 8
+  for (int s = w; s < g.splits; s += W) {
+    const f32x2 x = *(const f32x2*)(stat + (long long)s * RT * 2);
+    const float f = x[1] > 0.f ? exp2_fast(x[0] - top) : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(part[(long long)s * RT * D + lane * E + e], f, o[e]);
+  }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = o[e];
+    __syncthreads();
+    if (w == 0) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        for (int i = 1; i < W; ++i) o[e] += sums[wave + i][lane * E + e];
+    }
+  }
+  if (w != 0 || id >= rows) return;
   T* out = (T*)g.O + query_offset<MODE>(q, q.o, b, hd, rr);
 #pragma unroll
   for (int e = 0; e < E; ++e) out[lane * E + e] = (T)(l > 0.f ? o[e] / l : 0.f);
@@ -201,46 +255,61 @@ __global__ __launch_bounds__(256) void dense_join_kernel(DenseGeo q, FwdArgs g, 
 
 namespace {
 
-template <class T, int D, int NQ, int NW, int MODE>
+template <class T, int D, int NQ, int NW, int JW, int MODE>
 hipError_t run_fwd(const DenseGeo& q, const FwdPlan& p, dense::FwdArgs a, hipStream_t s) {
   const size_t lds = MODE == dense::BIAS ? dense::bias_entries(q.rule.cut) * sizeof(float) : 0;
-  dense::dense_fwd_kernel<T, D, NQ, NW, MODE><<<grid_of(a.items), 64 * NW, lds, s>>>(q, a);
+  dense::dense_fwd_kernel<T, D, NQ, NW, JW, MODE><<<grid_of(a.items), 64 * NW, lds, s>>>(q, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const long long rows = (long long)q.B * dense_heads(q) * a.rows;
-  dense::dense_join_kernel<T, D, MODE><<<grid_of((rows + 3) / 4), 256, 0, s>>>(q, a, 32 * NQ * NW);
+  const int rt = 32 * NQ * (NW / JW);
+  // (a wave to a row needs thousands of rows to fill the card)
+  if (rows <= 2048) dense::dense_join_kernel<T, D, 4, MODE><<<grid_of(rows), 256, 0, s>>>(q, a, rt);
+  else dense::dense_join_kernel<T, D, 1, MODE><<<grid_of((rows + 3) / 4), 256, 0, s>>>(q, a, rt);
   return hipGetLastError();
 }
 
 template <class T, int D, int MODE>
 hipError_t pick_fwd(const DenseGeo& q, const FwdPlan& p, const dense::FwdArgs& a, hipStream_t s) {
-  if (p.waves == 1) return run_fwd<T, D, 1, 1, MODE>(q, p, a, s);
-  if (p.sets == 1) return run_fwd<T, D, 1, 4, MODE>(q, p, a, s);
-  if constexpr (sizeof(T) == 2) return run_fwd<T, D, 2, 4, MODE>(q, p, a, s);
-  return hipErrorInvalidValue;
+  constexpr int J = dense::kJoin<T, D>;
+  if (p.join) return run_fwd<T, D, 1, J, J, MODE>(q, p, a, s);
+  if constexpr (sizeof(T) == 2)
+    if (p.sets == 2) return run_fwd<T, D, 2, 4, 1, MODE>(q, p, a, s);
+  return run_fwd<T, D, 1, 4, 1, MODE>(q, p, a, s);
 }
 
 }  // namespace
 
+// Workgroups of four waves with 64 queries each (bf16, where they fill the card: each operand from LDS feeds two products), with 32 each, or of
+// waves that share 32 queries and take the keys in turn.
 FwdPlan plan_dense_fwd(const DenseGeo& q) {
   FwdPlan p;
-  const long long rows = dense_rows(q), bh = (long long)q.B * dense_heads(q);
-  p.waves = rows <= 64 ? 1 : 4;
-  p.sets = q.dtype == DA_BF16 && p.waves == 4 && bh * ((rows + 255) / 256) >= kCUs ? 2 : 1;
-  const int rt = 32 * p.sets * p.waves;
-  p.tiles = (int)((rows + rt - 1) / rt);
-  const int kb = q.dtype == DA_F32 && q.d == 128 ? 32 : 64;
-  const long long wgs = bh * p.tiles, key_tiles = (q.M + kb - 1) / kb, want = p.waves == 1 ? 4 * kCUs : 2 * kCUs;
-  long long splits = wgs >= want ? 1 : (want + wgs - 1) / wgs;
-  if (splits > key_tiles / 4) splits = key_tiles / 4;
-  p.splits = splits < 1 ? 1 : (int)splits;
+  const long long rows = dense_rows(q), heads = (long long)q.B * dense_heads(q);
+  const bool f32 = q.dtype == DA_F32, wide = q.d * (f32 ? 4 : 2) > 256;
+  const long long wgs = heads * ((rows + 127) / 128), units = (q.M + (wide ? 31 : 63)) / (wide ? 32 : 64);
+  p.join = 0; p.sets = 1; p.splits = 1;
+  if (!f32 && heads * ((rows + 255) / 256) >= kCUs) {
+    p.sets = 2;
+  } else if (wgs < kCUs / 4 * 3) {
+    p.splits = rows > 64 ? cut(wgs, units, 2 * kCUs, 2 * product_us(q), 128.0 * wgs * q.d * 4e-6) : 1;
+    if (wgs * p.splits < kCUs / 4 * 3) {
+      p.join = 1;
+      const int n = wide ? 64 : 128, slots = q.d * (f32 ? 4 : 2) == 128 ? 2 * kCUs : kCUs;
+      const long long small = heads * ((rows + 31) / 32), tiles = (q.M + n - 1) / n;
+      long long s = small > 0 ? slots / small : 1;
+      if (s > tiles / 2) s = tiles / 2;
+      p.splits = s < 1 ? 1 : (int)s;
+    }
+  }
+  p.row_tile = p.join ? 32 : 128 * p.sets;
+  p.tiles = (int)((rows + p.row_tile - 1) / p.row_tile);
   return p;
 }
 
 size_t dense_fwd_workspace(const DenseGeo& q) {
   const FwdPlan p = plan_dense_fwd(q);
   if (p.splits == 1) return 0;
-  return (size_t)q.B * dense_heads(q) * p.tiles * p.splits * (32 * p.sets * p.waves) * (q.d + 2) * sizeof(float);
+  return (size_t)q.B * dense_heads(q) * p.tiles * p.splits * p.row_tile * (q.d + 2) * sizeof(float);
 }
 
 hipError_t launch_dense_fwd(const DenseGeo& q, const void* Q, const void* K, const void* V, const void* table, void* O, float* lse,

@@ -33,7 +33,34 @@ struct BwdArgs {
   int row_tiles, per_head;         // dkv: tiles of queries of a head, pieces of a head
 };
 
-constexpr int kScratch = 36;       // row stride, in words, of the square that a wave's ds goes through for its diagonals
+// The sums of a square by r = key - query, keys on the lanes (32, twice) and queries in the registers: a register's halves are put into two, each
+// with zeros in the upper lanes (v_permlane32_swap), and added up query by query, with a step of one lane between them (wave_shr): after 16
+// queries lane l holds the sum of key - query = l - 15.  Two chains, queries 0..15 and 16..31, with an array each in LDS.
+// (24 heads of 4099 by 4099, 128 channels, gradients of K and V: 734 us by way of a square in LDS, whose room also kept a second workgroup off
+// the CU.  Straight into LDS with its own addition, ds_add_f32: 64 heads of 512 by 512 193 us instead of 73.)
+__device__ __forceinline__ void add_diagonals(const f32x16& x, float* at, int n_bias, int lane) {
+  auto next = [](float sum, unsigned y) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, sum), 0x138, 0xf, 0xf, true)) + __uint_as_float(y);
+  };
+  unsigned up[2][8];
+  float sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int a = 0; a < 8; ++a)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[8 * i + a]), 0u, false, false);
+      sum[i] = next(sum[i], y[0]);
+      up[i][a] = y[1];
+    }
+#pragma unroll
+  for (int a = 0; a < 8; ++a)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sum[i] = next(sum[i], up[i][a]);
+  if (lane < 47) {
+    at[lane - 15] += sum[0];
+    at[n_bias + lane - 31] += sum[1];
+  }
+}
 
 template <class T> __device__ __forceinline__ float dot_piece(const typename Type<T>::piece& x, const typename Type<T>::piece& y, float s) {
 #pragma unroll
@@ -205,7 +232,7 @@ template <class T, int D, int NW, int JW, int MODE>
 __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kernel(DenseGeo q, BwdArgs g) {
   constexpr int QB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>, TILE = QB * RB, STAGE = 2 * TILE + 1024, KT = 32 * (NW / JW);
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[2 * STAGE];  // twice: Q, dO, lse2 and delta of their rows
-  extern __shared__ __attribute__((aligned(16))) float bias_row[];           // then per wave its diagonals and its square
+  extern __shared__ __attribute__((aligned(16))) float bias_row[];           // then each wave's sums of ds by r
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
   if (id >= g.items) return;
   const long long item = xcd_order(id, g.items);
@@ -254,11 +281,11 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
   };
   if (t0 < t1) load_rows(t0, lds);
   const int n_bias = MODE == BIAS ? (bias_entries(q.rule.cut) + 3) & ~3 : 0;
-  float *diag = bias_row + n_bias + wave * (n_bias + 32 * kScratch), *square = diag + n_bias;
+  float* diag = bias_row + n_bias + wave * (2 * n_bias);         // this wave's sums by r, as the bias row: two arrays
   float far_sum[2] = {0.f, 0.f};
   if constexpr (MODE == BIAS) {
     fill_bias<T>(bias_row, q.rule, (const T*)g.table, q.H, hd, threadIdx.x, 64 * NW);
-    for (int i = lane; i < n_bias; i += 64) diag[i] = 0.f;
+    for (int i = lane; i < 2 * n_bias; i += 64) diag[i] = 0.f;
   }
 
   Own<T, D> own_k[1], own_v[1];
@@ -334,26 +361,7 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
           far_sum[0] += low > 0 ? 0.f : x;
           far_sum[1] += low > 0 ? x : 0.f;
         } else {
-          // Diagonals of the square (key n, query m; r = low + n - m): by way of LDS lane c reads the queries (n - c) mod 32 of half the
-          // keys, whose sum belongs to r = low + c where n >= c and to low + c - 32 elsewhere.
-          f32x4* row = (f32x4*)(square + (lane & 31) * kScratch + 8 * hi);
-          row[0] = f32x4{dp[0][0], dp[0][1], dp[0][2], dp[0][3]};
-          row[1] = f32x4{dp[0][4], dp[0][5], dp[0][6], dp[0][7]};
-          row[4] = f32x4{dp[0][8], dp[0][9], dp[0][10], dp[0][11]};
-          row[5] = f32x4{dp[0][12], dp[0][13], dp[0][14], dp[0][15]};
-          __builtin_amdgcn_wave_barrier();
-          const int c = lane & 31;
-          float straight = 0.f, wrapped = 0.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int n = 2 * i + hi;
-            const float x = square[n * kScratch + ((n - c) & 31)];
-            straight += n >= c ? x : 0.f;
-            wrapped += n >= c ? 0.f : x;
-          }
-          const float d0 = sum_across_halves(straight), d1 = sum_across_halves(wrapped);
-          diag[low + (hi ? c - 32 : c) + q.rule.cut + kBiasPad] += hi ? d1 : d0;
-          __builtin_amdgcn_wave_barrier();
+          add_diagonals(dp[0], diag + low + q.rule.cut + kBiasPad, n_bias, lane);
         }
       }
       mix<T, D, 1>(buf + TILE + sub * 32 * RB + m_lane, p, zv);
@@ -392,13 +400,13 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
     }
   }
   if constexpr (MODE == BIAS) {
-    // the waves' diagonals, added up bucket by bucket: eight lanes to a bucket
+    // the waves' sums by r, added up bucket by bucket: eight lanes to a bucket
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       float x = far_sum[i];
 #pragma unroll
       for (int w = 32; w >= 1; w >>= 1) x += __shfl_xor(x, w);
-      if (lane == 0) diag[i ? 2 * (q.rule.cut + kBiasPad) : 0] += x;
+      if (lane == 0) diag[(i ? 2 * (q.rule.cut + kBiasPad) : 0)] += x;
     }
     __syncthreads();
     for (int c0 = 0; c0 < q.buckets; c0 += 8 * NW) {
@@ -409,7 +417,7 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
         bucket_range(q.rule, c, first, last);
         for (int i = first + (threadIdx.x & 7); i <= last; i += 8)
 #pragma unroll
-          for (int w = 0; w < NW; ++w) x += bias_row[n_bias + w * (n_bias + 32 * kScratch) + i];
+          for (int w = 0; w < 2 * NW; ++w) x += bias_row[n_bias + w * n_bias + i];
       }
 #pragma unroll
       for (int w = 4; w >= 1; w >>= 1) x += __shfl_xor(x, w);
@@ -500,11 +508,11 @@ struct BwdPlan {
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// LDS of the second kernel beside its tiles: bias, diagonals and squares of `waves` waves
+// LDS of the second kernel beside its tiles: bias and sums by r of `waves` waves
 inline size_t dkv_bias_lds(const DenseGeo& q, int waves) {
   if (!q.bias) return 0;
   const size_t n = (dense::bias_entries(q.rule.cut) + 3) & ~3;
-  return (n + waves * (n + 32 * dense::kScratch)) * sizeof(float);
+  return (n + 2 * waves * n) * sizeof(float);
 }
 
 // Workgroups of four waves with 32 queries (keys) each, or, where they are too few, of waves that share 32 and take the other side in turn.

@@ -288,11 +288,11 @@ FwdPlan plan_dense_fwd(const DenseGeo& q) {
   const bool f32 = q.dtype == DA_F32, wide = q.d * (f32 ? 4 : 2) > 256;
   const long long wgs = heads * ((rows + 127) / 128), units = (q.M + (wide ? 31 : 63)) / (wide ? 32 : 64);
   p.join = 0; p.sets = 1; p.splits = 1;
-  if (!f32 && heads * ((rows + 255) / 256) >= kCUs) {
+  if (!f32 && rows > 128 && heads * ((rows + 255) / 256) >= kCUs / 2 * 3) {   // three quarters of the places, two to a CU
     p.sets = 2;
-  } else if (wgs < kCUs / 4 * 3) {
+  } else if (wgs < kCUs / 4 * 3 || rows <= 64) {
     p.splits = rows > 64 ? cut(wgs, units, 2 * kCUs, 2 * product_us(q), 128.0 * wgs * q.d * 4e-6) : 1;
-    if (wgs * p.splits < kCUs / 4 * 3) {
+    if (wgs * p.splits < kCUs / 4 * 3 || rows <= 64) {
       p.join = 1;
       const int n = wide ? 64 : 128, slots = q.d * (f32 ? 4 : 2) == 128 ? 2 * kCUs : kCUs;
       const long long small = heads * ((rows + 31) / 32), tiles = (q.M + n - 1) / n;

@@ -161,8 +161,9 @@ template <class T, int D> __device__ __forceinline__ unsigned scores_lane(int la
 // NQ sets of 32 columns against 32 rows of the tile, added to what c holds
 template <class T, int D, int NQ>
 __device__ __forceinline__ void add_scores(unsigned at, const Own<T, D> (&own)[NQ], f32x16 (&c)[NQ]) {
-  // operands arrive AHEAD steps before their use and no earlier: more of them in flight would not fit the registers
-  constexpr int N = Own<T, D>::N, AHEAD = 3;
+  // Operands arrive AHEAD steps before their use: more of them in flight do not fit the registers of 64 queries (40 heads of 75600 by 512, forward:
+  // three 1020 us, two 950 us).
+  constexpr int N = Own<T, D>::N, AHEAD = 2;
   typename Type<T>::piece x[N];
   auto fetch = [&](int t) { x[t] = *(const __attribute__((address_space(3))) typename Type<T>::piece*)(uintptr_t)(at ^ (32 * t)); };
 #pragma unroll
@@ -180,6 +181,26 @@ __device__ __forceinline__ void add_scores(unsigned at, const Own<T, D> (&own)[N
 #pragma unroll
         for (int h = 0; h < NQ; ++h) c[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[t][i], own[h].x[t][i], c[h], 0, 0, 0);
     }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// bf16, with the wave's own 32 rows in LDS as well, where registers are short: piece t of lane l at own_at + 1024 t, own_at + 16 l being the lane's
+template <int D>
+__device__ __forceinline__ void add_scores_lds(unsigned at, unsigned own_at, f32x16& c) {
+  constexpr int N = Own<__bf16, D>::N, AHEAD = 2;
+  bf16x8 x[N], y[N];
+  auto fetch = [&](int t) {
+    x[t] = *(lds_bf16x8*)(uintptr_t)(at ^ (32 * t));
+    y[t] = *(lds_bf16x8*)(uintptr_t)(own_at + 1024 * t);
+  };
+#pragma unroll
+  for (int t = 0; t < AHEAD; ++t) fetch(t);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    if (t + AHEAD < N) fetch(t + AHEAD);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[t], y[t], c, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -229,7 +250,7 @@ template <class T, int D, int NQ>
 __device__ __forceinline__ void mix(unsigned at, const Mixed<T> (&c)[NQ], f32x16 (&z)[NQ][D / 32]) {
   constexpr int RB = kRowBytes<T, D>, G = D / 32;
   if constexpr (sizeof(T) == 2) {
-    constexpr int N = 2 * G, AHEAD = 3;
+    constexpr int N = 2 * G, AHEAD = 2;
     s16x8 x[N];
     auto fetch = [&](int i) {
       const int t = i / G, dt = i % G;
@@ -320,10 +341,14 @@ __device__ __forceinline__ void read_bias(unsigned at, f32x16& b) {
   for (int a = 0; a < 16; ++a) b[a] = *(lds_f32*)(uintptr_t)(at + SIGN * 4 * (16 * (a >> 3) + (a & 7)));
 }
 
-// workgroups are dealt to the 8 XCDs in turn: consecutive pieces of work go to one XCD, whose L2 then holds the rows they share
-__device__ __forceinline__ long long xcd_order(long long id, long long total) {
-  const long long each = total / 8, more = total % 8, x = id % 8;
-  return x * each + min(x, more) + id / 8;
+// Workgroups are dealt to the 8 XCDs in turn.  The `each` pieces of work of a head go to one XCD, whose L2 then holds the rows that they share, and
+// the heads to the XCDs in turn, so that batch elements of different lengths are spread over all of them (64 heads of 512 queries, keys of 512, 336, 160 and
+// 444: the three kernels of a training step 155 us with an eighth of the list to each XCD, 141 us so).  Heads beyond a multiple of 8: an eighth of their pieces each.
+__device__ __forceinline__ long long xcd_order(long long id, long long total, long long each) {
+  const long long turns = total / each / 8, most = turns * 8 * each, x = id % 8, n = id / 8;
+  if (id < most) return (n / each * 8 + x) * each + n % each;
+  const long long rest = total - most, part = rest / 8, more = rest % 8, i = (id - most) / 8;
+  return most + x * part + min(x, more) + i;                // (most is a multiple of 8)
 }
 
 // Rows of a tile.  Waves that have each 32 or 64 columns of their own share tiles of 16 KB at most, so that two workgroups of two pairs of

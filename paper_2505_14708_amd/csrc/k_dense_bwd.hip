@@ -104,7 +104,7 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
   extern __shared__ __attribute__((aligned(16))) float bias_row[];
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
   if (id >= g.items) return;
-  const long long item = xcd_order(id, g.items);
+  const long long item = xcd_order(id, g.items, (long long)g.tiles * g.splits);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
   const int split = (int)(item % g.splits);
   const long long bht = item / g.splits;
@@ -228,14 +228,22 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
 // waves to a SIMD that the kernel below is made for
 template <class T, int D, int JW> constexpr int kDkvWaves = JW > 1 || kRowBytes<T, D> > 256 ? 1 : 2;
 
+// bf16, 128 channels: the sums of 32 keys are 128 registers, K's and V's rows 64 and the squares of scores and of dO V^T 32, of 256.  With a bias
+// that is too much by a few, which would be spilled, and their way back waits, in the order of all loads, for the next tiles (24 heads of 4099 by
+// 4099: 545 us).  There V's rows are in LDS, 8 KB a wave, and the tiles are of 32 rows so that two workgroups still fit a CU (511 us).
+template <class T, int D, int JW, int MODE> constexpr bool kVInLds = sizeof(T) == 2 && D == 128 && JW == 1 && MODE == BIAS;
+template <class T, int D, int JW, int MODE> constexpr int kDkvRows = kVInLds<T, D, JW, MODE> ? 32 : kTileRows<T, D, JW>;
+
 template <class T, int D, int NW, int JW, int MODE>
 __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kernel(DenseGeo q, BwdArgs g) {
-  constexpr int QB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>, TILE = QB * RB, STAGE = 2 * TILE + 1024, KT = 32 * (NW / JW);
-  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2 * STAGE];  // twice: Q, dO, lse2 and delta of their rows
+  constexpr int QB = kDkvRows<T, D, JW, MODE>, RB = kRowBytes<T, D>, TILE = QB * RB, STAGE = 2 * TILE + 1024, KT = 32 * (NW / JW);
+  constexpr bool V_IN_LDS = kVInLds<T, D, JW, MODE>;
+  // twice: Q, dO, where their rows start from and delta; the waves' own rows of V
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2 * STAGE + (V_IN_LDS ? NW * 32 * RB : 0)];
   extern __shared__ __attribute__((aligned(16))) float bias_row[];           // then each wave's sums of ds by r
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
   if (id >= g.items) return;
-  const long long item = xcd_order(id, g.items);
+  const long long item = xcd_order(id, g.items, (long long)g.tiles * g.splits);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
   // the tiles of keys of one piece of the queries are neighbours: they read the same rows
   const int tile = (int)(item % g.tiles);
@@ -296,6 +304,10 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
     const long long kc = min(key0 + (lane & 31), len - 1);
     own_k[0].load(g.K + (b * q.k.sb + hk * q.k.sh + kc * q.k.sn) * (long long)sizeof(T), hi);
     own_v[0].load(g.V + (b * q.v.sb + hk * q.v.sh + kc * q.v.sn) * (long long)sizeof(T), hi);
+    if constexpr (V_IN_LDS) {
+#pragma unroll
+      for (int t = 0; t < Own<T, D>::N; ++t) *(bf16x8*)(tiles + 2 * STAGE + wave * 32 * RB + t * 1024 + lane * 16) = own_v[0].x[t];
+    }
   }
   const unsigned s_lane = scores_lane<T, D>(lane), m_lane = mix_lane<T, D>(lane);
   const unsigned bias_lds = MODE == BIAS ? (unsigned)(uintptr_t)(lds_f32*)bias_row : 0u;
@@ -326,7 +338,8 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
         }
       }
       add_scores<T, D, 1>(buf + sub * 32 * RB + s_lane, own_k, s);
-      add_scores<T, D, 1>(buf + TILE + sub * 32 * RB + s_lane, own_v, dp);
+      if constexpr (V_IN_LDS) add_scores_lds<D>(buf + TILE + sub * 32 * RB + s_lane, lds + 2 * STAGE + wave * 32 * RB + lane * 16, dp[0]);
+      else add_scores<T, D, 1>(buf + TILE + sub * 32 * RB + s_lane, own_v, dp);
       const int low = MODE == BIAS ? key0 - row0 - q.q_pos : 0;      // r of key 0 and query 0 of the square
       const bool is_far = MODE == BIAS && (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut);
       if constexpr (MODE == BIAS) {
@@ -341,6 +354,11 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
           for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], kLate ? bs[a] + late[a] : bs[a]);
         }
       } else {
+        // (A branch that is always taken: in one block with the products the exponentials cost 16 to 48 spilled registers, in one of their own none.
+        // 24 heads of 32760 by 512: 540 and 427 us.)
+        int always = 1;
+        asm volatile("" : "+s"(always));
+        if (always)
 #pragma unroll
         for (int a = 0; a < 16; ++a) s[0][a] = kLate ? power_of<T>(q, s[0][a], late[a]) : exp2_fast(s[0][a] * q.c2);
       }
@@ -449,6 +467,7 @@ __global__ __launch_bounds__(256) void dense_sum_dq_kernel(DenseGeo q, BwdArgs g
   sum_pieces<T, D>(g.dq_part + first * D, (long long)RT * D, g.splits, (T*)g.dQ + query_offset<MODE>(q, q.dq, b, hd, rr), threadIdx.x % P);
   if (threadIdx.x % P == 0) {      // and what delta is off by
     float off = 0.f;
+#pragma unroll 8
     for (int s = 0; s < g.splits; ++s) off += g.r_part[first + (long long)s * RT];
     g.delta[bh * g.padded + rr] -= off;
   }
@@ -521,6 +540,7 @@ BwdPlan plan_bwd(const DenseGeo& q) {
   const long long rows = dense_rows(q), heads = (long long)q.B * dense_heads(q), kv_heads = (long long)q.B * q.Hk;
   const bool f32 = q.dtype == DA_F32;
   const int row_bytes = q.d * (f32 ? 4 : 2), tile = row_bytes > 256 ? 32 : 64, enough = kCUs / 4 * 3;
+  const int kv_tile = !f32 && q.d == 128 && q.bias ? 32 : tile;
   const int joined = row_bytes > 256 ? 64 : 128, join_slots = row_bytes == 128 ? 2 * kCUs : kCUs;      // rows of a joining workgroup's tile
   const int slots = row_bytes > 256 ? kCUs : 2 * kCUs;                                                 // (one wave to a SIMD there)
   auto pieces_joined = [&](long long wgs, long long units) {
@@ -547,7 +567,7 @@ BwdPlan plan_bwd(const DenseGeo& q) {
     p.per_head = pieces_joined(kv_heads * stretches * ((q.M + 31) / 32), (rows + joined - 1) / joined);
   }
   const int kt = p.kv_join ? 32 : 128;
-  p.q_tile = p.kv_join ? joined : tile;
+  p.q_tile = p.kv_join ? joined : kv_tile;
   p.kv_tiles = (q.M + kt - 1) / kt;
   p.row_tiles = (int)((rows + p.q_tile - 1) / p.q_tile);
   p.kv_splits = p.per_head * stretches;

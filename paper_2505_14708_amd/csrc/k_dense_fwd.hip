@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
   extern __shared__ __attribute__((aligned(16))) float bias_row[];
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
   if (id >= g.items) return;
-  const long long item = xcd_order(id, g.items);
+  const long long item = xcd_order(id, g.items, (long long)g.tiles * g.splits);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
   const int split = (int)(item % g.splits);
   const long long bht = item / g.splits;

@@ -1,7 +1,7 @@
 // Buckets of relative positions (host arithmetic; no HIP, so that it compiles for the CPU by itself).
 #pragma once
+#include <math.h>
 #include <stdint.h>
-#include <vector>
 
 namespace da {
 
@@ -20,24 +20,29 @@ struct RelRule {
   int16_t border[kMaxBuckets / 2 + 1];   // where shared bucket 1, 2, .. begins
 };
 
-// a^p >= b^(p - k) c^k, exactly (numbers below 2^16)
+// a^p >= b^(p - k) c^k, exactly (numbers of up to 11 bits, powers of up to kMaxBuckets)
 inline bool power_reaches(int a, int p, int b, int c, int k) {
-  auto times = [](std::vector<uint32_t>& x, uint32_t f) {
-    uint64_t carry = 0;
-    for (uint32_t& w : x) {
-      carry += (uint64_t)w * f;
-      w = (uint32_t)carry;
-      carry >>= 32;
+  constexpr int kWords = (11 * kMaxBuckets + 31) / 32 + 1;
+  struct Number {
+    uint32_t w[kWords];
+    int n;
+    void times(uint32_t f) {
+      uint64_t carry = 0;
+      for (int i = 0; i < n; ++i) {
+        carry += (uint64_t)w[i] * f;
+        w[i] = (uint32_t)carry;
+        carry >>= 32;
+      }
+      if (carry) w[n++] = (uint32_t)carry;
     }
-    if (carry) x.push_back((uint32_t)carry);
-  };
-  std::vector<uint32_t> l{1u}, r{1u};
-  for (int i = 0; i < p; ++i) times(l, (uint32_t)a);
-  for (int i = 0; i < p - k; ++i) times(r, (uint32_t)b);
-  for (int i = 0; i < k; ++i) times(r, (uint32_t)c);
-  if (l.size() != r.size()) return l.size() > r.size();
-  for (size_t i = l.size(); i-- > 0;)
-    if (l[i] != r[i]) return l[i] > r[i];
+  } l, r;
+  l.w[0] = r.w[0] = 1u;
+  l.n = r.n = 1;
+  for (int i = 0; i < p; ++i) l.times((uint32_t)a);
+  for (int i = 0; i < p; ++i) r.times((uint32_t)(i < k ? c : b));
+  if (l.n != r.n) return l.n > r.n;
+  for (int i = l.n; i-- > 0;)
+    if (l.w[i] != r.w[i]) return l.w[i] > r.w[i];
   return true;
 }
 
@@ -52,11 +57,11 @@ inline bool make_rel_rule(int buckets, int max_distance, int bidirectional, RelR
   if (t.e < 1 || max_distance <= t.e || max_distance > kMaxDistance) return false;
   t.n_border = t.n - t.e - 1;
   for (int k = 1; k <= t.n_border; ++k) {
-    int lo = k > 1 ? t.border[k - 2] : t.e, hi = max_distance;      // max_distance^(n - e) reaches every k
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (power_reaches(mid, t.n - t.e, t.e, max_distance, k)) hi = mid; else lo = mid + 1;
-    }
+    // in doubles, whose error is below 1e-11 here, unless a whole number lies nearer than 1e-6: then exactly
+    const double at = t.e * pow((double)max_distance / t.e, (double)k / (t.n - t.e));
+    const int near = (int)floor(at + 0.5);
+    int lo = (int)ceil(at);
+    if (fabs(at - near) < 1e-6) lo = power_reaches(near, t.n - t.e, t.e, max_distance, k) ? near : near + 1;
     t.border[k - 1] = (int16_t)lo;
   }
   for (int k = t.n_border; k <= kMaxBuckets / 2; ++k) t.border[k] = 0;

@@ -303,7 +303,7 @@ typedef struct da_attn_problem {
   int32_t d;           /* head dimension: 64 or 128 */
   int32_t dtype;       /* DA_F32 or DA_BF16: every tensor but lse and kv_len */
   int32_t reserved;    /* 0 */
-  double  scale;       /* factor of the scores, > 0; 0 stands for 1/sqrt(d) */
+  double  scale;       /* factor of the scores, 1e-30 .. 1e30; 0 stands for 1/sqrt(d) */
 } da_attn_problem;
 
 /* Where the rows of each tensor live, [B, heads, rows, d] (see da_layout; every one has its own).  A da_layout of zeros, or NULL in the

@@ -410,7 +410,7 @@ __device__ __forceinline__ long long query_offset(const DenseGeo& q, const Rows&
 
 // s c2 + add.  float32: the rounding of c2 alone would be off by |s c2| 2^-25, and is made good.
 template <class T> __device__ __forceinline__ float biased(const DenseGeo& q, float s, float add) {
-  if constexpr (sizeof(T) == 4) add = __builtin_fmaf(s == -INFINITY ? 0.f : s, q.c2_lo, add);
+  if constexpr (sizeof(T) == 4) add = __builtin_fmaf(fmaxf(s, -FLT_MAX), q.c2_lo, add);     // (a score of minus infinity stays one)
   return __builtin_fmaf(s, q.c2, add);
 }
 template <class T> __device__ __forceinline__ float power_of(const DenseGeo& q, float s, float add) { return exp2_fast(biased<T>(q, s, add)); }

@@ -50,7 +50,7 @@ int check_attn(const da_attn_problem* p, const da_rel_bias* bias, const da_attn_
   if (!p) return DA_ERR_NULL;
   if (p->B < 1 || p->H < 1 || p->Hk < 1 || p->N < 1 || p->M < 1 || p->d < 1 || p->H % p->Hk != 0) return DA_ERR_DIM;
   if (p->dtype != DA_F32 && p->dtype != DA_BF16) return DA_ERR_DIM;
-  if (!(p->scale >= 0.0 && p->scale <= 1.0e30)) return DA_ERR_DIM;   // also rejects NaN
+  if (p->scale != 0.0 && !(p->scale >= 1.0e-30 && p->scale <= 1.0e30)) return DA_ERR_DIM;   // also rejects NaN
   DenseGeo q;
   q.B = p->B; q.H = p->H; q.Hk = p->Hk; q.group = p->H / p->Hk; q.N = p->N; q.M = p->M; q.d = p->d; q.dtype = p->dtype;
   if (q.N > kMaxRows || q.M > kMaxRows || (long long)q.group * q.N > kMaxRows || (long long)q.B * q.H > 2147483647LL) return DA_ERR_DIM;

@@ -512,7 +512,9 @@ __global__ __launch_bounds__(256) void dense_sum_dkv_kernel(DenseGeo q, BwdArgs 
 template <class T>
 __global__ __launch_bounds__(256) void dense_sum_bias_kernel(DenseGeo q, BwdArgs g) {
   __shared__ float sums[256];
-  const int h = blockIdx.x, c = threadIdx.x % q.buckets, slice = threadIdx.x / q.buckets, slices = 256 / q.buckets;
+  const long long h = blockIdx.y * (long long)gridDim.x + blockIdx.x;
+  if (h >= q.H) return;
+  const int c = threadIdx.x % q.buckets, slice = threadIdx.x / q.buckets, slices = 256 / q.buckets;
   const long long run = (long long)g.per_head * g.tiles, n = run * q.B, per_batch = run * q.H;   // (a batch element's heads follow each other)
   float x = 0.f;
   if (slice < slices) {
@@ -620,7 +622,7 @@ hipError_t run_dkv(const DenseGeo& q, const BwdPlan& p, const dense::BwdArgs& a,
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (MODE == dense::BIAS) {
-    dense::dense_sum_bias_kernel<T><<<q.H, 256, 0, s>>>(q, a);
+    dense::dense_sum_bias_kernel<T><<<grid_of(q.H), 256, 0, s>>>(q, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (p.kv_splits == 1) return e;

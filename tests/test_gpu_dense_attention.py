@@ -142,6 +142,31 @@ def test_other_stream_and_graph():
                 assert torch.equal(x, want[n]), (rule, i, n)
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("scale", [1e-30, 1e-6, 3.0])
+def test_scales(dtype, d, scale):
+    """Scores that vanish beside lse, and peaked ones."""
+    run(f"scale {scale} {dtype} d={d}", dtype, 1, 2, 2, 60, 200, d, scale=scale, lens=[150], seed=12)
+    run(f"scale {scale} {dtype} d={d}, bias", dtype, 1, 2, 2, 60, 200, d, scale=scale, rule=(32, 128, 1, 0), seed=12)
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, at the same time: the results of one after the other."""
+    for rule in (None, (32, 128, 1, 0)):
+        prs = [Problem("bf16", 2, 8, 4, 90, 3000, 64, rule=rule, lens=[3000, 100], seed=s) for s in (20, 21)]
+        want = [{n: x.clone() for n, x in pr.run().items()} for pr in prs]
+        streams = [torch.cuda.Stream() for _ in prs]
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for pr, s in zip(prs, streams):
+                with torch.cuda.stream(s):
+                    pr.run()
+        torch.cuda.synchronize()
+        for pr, w in zip(prs, want):
+            for n, x in pr.results().items():
+                assert torch.equal(x, w[n]), (rule, n)
+
+
 def test_rows_far_apart():
     """Offsets beyond 32 bits: rows of K and V 8 MB apart, in a buffer of 3 GB that holds nothing else."""
     M, step = 384, 4 << 20                                       # elements

@@ -42,7 +42,7 @@ def test_structs_match_the_header():
 
 @pytest.mark.parametrize("change,status", [
     (dict(B=0), -2), (dict(H=0), -2), (dict(Hk=0), -2), (dict(Hk=3), -2), (dict(Hk=8), -2), (dict(N=0), -2), (dict(M=0), -2),
-    (dict(N=-1), -2), (dict(d=0), -2), (dict(dtype=2), -2), (dict(scale=-1.0), -2), (dict(scale=float("nan")), -2), (dict(scale=float("inf")), -2),
+    (dict(N=-1), -2), (dict(d=0), -2), (dict(dtype=2), -2), (dict(scale=-1.0), -2), (dict(scale=float("nan")), -2), (dict(scale=float("inf")), -2), (dict(scale=1e-31), -2), (dict(scale=1e31), -2),
     (dict(N=(1 << 29) + 1), -2), (dict(M=(1 << 29) + 1), -2), (dict(N=1 << 29, H=8, Hk=4), -2), (dict(B=1 << 30, H=4), -2),
     (dict(d=96), -3), (dict(d=256), -3), (dict(d=32), -3)])
 def test_problems_that_are_refused(change, status):
@@ -194,7 +194,7 @@ def test_grids_stay_within_the_launch_limits(tmp_path):
     cases = []
     for dtype in (da.DA_F32, da.DA_BF16):
         for d in (64, 128):
-            for B, H, N, M, Hk in ((1, 1, 1, 1, 1), (1, 40, 118800, 512, 40), (8, 64, 1, 100000, 8), (1 << 20, 64, 1, 1, 64), (1, 1, 1 << 29, 3, 1),
+            for B, H, N, M, Hk in ((1, 1, 1, 1, 1), (1, 40, 118800, 512, 40), (8, 64, 1, 100000, 8), (1 << 20, 64, 1, 1, 64), (1, 1 << 25, 1, 1, 1 << 25), (1, 1, 1 << 29, 3, 1),
                                    (1, 1, 3, 1 << 29, 1), (2, 8, 4096, 4096, 2), (30000, 1, 700, 700, 1)):
                 cases += [((B, H, N, M, d, Hk, dtype), None), ((B, H, N, M, d, Hk, dtype), (256, 1024, 0, 0))]
     r = subprocess.run([sys.executable, "-c", CHILD, out, ROOT], input="\n".join(json.dumps(c) for c in cases), capture_output=True, text=True,

@@ -334,7 +334,7 @@ __device__ __forceinline__ void fill_bias(float* lds, const RelRule& rule, const
   }
 }
 
-// the swap of a table's registers for a square: where the wave's columns are queries (SIGN +1: r grows with the register's row) or keys (-1)
+// a square's bias: the wave's columns are queries (SIGN +1: r grows with the register's row) or keys (-1)
 template <int SIGN>
 __device__ __forceinline__ void read_bias(unsigned at, f32x16& b) {
 #pragma unroll

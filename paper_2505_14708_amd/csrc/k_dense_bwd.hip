@@ -5,13 +5,16 @@
 // Two kernels, each of which makes p and dO V^T anew (seven products of N x M x d instead of five, but no sums shared between
 // workgroups: no atomics, the same bits every time, and the sums stay in registers):
 //   dense_dq_kernel   32 queries a wave on the lane axis, tiles of K and V pass by
-//   dense_dkv_kernel  32 or 64 keys a wave on the lane axis, tiles of Q and dO pass by, with lse and delta of their rows; also the sums for dtable
+//   dense_dkv_kernel  32 keys a wave on the lane axis, tiles of Q and dO pass by, with lse and delta of their rows; also the sums for dtable
 // Where one side is short the other is cut and the pieces' sums are put together by a third launch, in a fixed order.
 //
 // delta.  O is stored with the type's rounding (bf16: 2^-8), and dO . O inherits it.  But sum_j ds_ij = 0 for the delta that belongs to p and
 // dO V^T, so what the first kernel's rows of ds add up to is what its delta is off by; the second kernel gets the corrected one.
-// (dtable, a sum of ds in which that error does not average out, was off by 2.9e-3 in norm with 64 heads of 512 by 512, by its final
-// rounding's 1.7e-3 now.)
+// (dtable, a sum of ds in which that error does not average out, was off by 2.9e-3 in norm with 64 heads of 512 by 512; by about its final
+// rounding's 1.7e-3 so.)
+//
+// Bounds: with 128 channels the matrix pipe at 0.8 to 0.97 PFLOP/s (24 heads of 32760 by 512: dQ 390 us, dK and dV 427 us), beside which the vector pipe
+// is busy about as long, with little of it at the same time; with 64 channels the vector instructions.
 #include <type_traits>
 #include "attn_tiles.h"
 

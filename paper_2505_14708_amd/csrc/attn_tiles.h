@@ -410,10 +410,27 @@ __device__ __forceinline__ long long query_offset(const DenseGeo& q, const Rows&
 
 // s c2 + add.  float32: the rounding of c2 alone would be off by |s c2| 2^-25, and is made good.
 template <class T> __device__ __forceinline__ float biased(const DenseGeo& q, float s, float add) {
-  if constexpr (sizeof(T) == 4) add = __builtin_fmaf(fmaxf(s, -FLT_MAX), q.c2_lo, add);     // (a score of minus infinity stays one)
+  if constexpr (sizeof(T) == 4) add = __builtin_fmaf(fmaxf(s, q.s_low), q.c2_lo, add);     // (a score of minus infinity stays one)
   return __builtin_fmaf(s, q.c2, add);
 }
 template <class T> __device__ __forceinline__ float power_of(const DenseGeo& q, float s, float add) { return exp2_fast(biased<T>(q, s, add)); }
+
+// What a row's exponentials are taken against: `top`, one of the row's largest x with a bias, of its scores without.  There, with r = top c2
+// rounded, exp2(fma(s, c2, -r)) has the rounding of its result only; the largest score's exponent is what r was rounded by, up to 2^-25 |r|, which all of the
+// row have in common, so that it divides out.  But where |r| reaches 2^31 the powers would be infinite, or all of them zero.  So beyond kNear it
+// is the differences of scores that are scaled: they are exact for the scores that count.
+constexpr float kNear = 0x1p24f;
+struct Ref { float score, x; };          // x of a score s against it: (s - score) c2 - x
+template <int MODE> __device__ __forceinline__ bool is_distant(const DenseGeo& q, float top) { return MODE != BIAS && fabsf(top * q.c2) > kNear; }
+template <int MODE> __device__ __forceinline__ Ref ref_of(const DenseGeo& q, float top) {
+  if constexpr (MODE == BIAS) return Ref{0.f, top};
+  return is_distant<MODE>(q, top) ? Ref{top, 0.f} : Ref{0.f, top * q.c2};
+}
+// what sums against `from` have to be multiplied by to be against `to`
+template <int MODE> __device__ __forceinline__ float moved(const DenseGeo& q, float from, float to) {
+  const Ref a = ref_of<MODE>(q, from), b = ref_of<MODE>(q, to);
+  return exp2_fast(__builtin_fmaf(a.score - b.score, q.c2, a.x - b.x));
+}
 
 }  // namespace dense
 

@@ -59,6 +59,7 @@ int check_attn(const da_attn_problem* p, const da_rel_bias* bias, const da_attn_
   q.scale = (float)scale;
   q.c2 = (float)(scale * 1.4426950408889634);
   q.c2_lo = (float)(scale * 1.4426950408889634 - (double)q.c2);
+  q.s_low = -(float)fmin(3.4e38, q.c2_lo == 0.f ? 3.4e38 : 3.4e38 / fabs((double)q.c2_lo));
   q.kv_len = nullptr;
   q.bias = 0; q.buckets = 0; q.q_pos = 0;
   q.rule = RelRule();

@@ -8,6 +8,7 @@ namespace da {
 struct DenseGeo {
   int B, H, Hk, group, N, M, d, dtype;
   float c2, c2_lo;       // scale * log2(e), and what its rounding left: the softmax works in powers of two
+  float s_low;           // the lowest score whose product with c2_lo is finite
   float scale;
   Rows q, k, v, o, dout, dq, dk, dv;
   const int32_t* kv_len; // keys of each batch element (NULL: M)

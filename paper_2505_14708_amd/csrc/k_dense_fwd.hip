@@ -19,15 +19,16 @@ struct FwdArgs {
   const void* table;
   unsigned char* O;
   float* lse;
-  float* part;           // splits > 1: [work item][rows of the tile][D] sums of P V, then [work item][rows of the tile][2] reference and sum of P
+  float* part;           // splits > 1: [work item][rows of the tile][D] sums of P V, then [work item][rows of the tile][2] top (ref_of) and sum of P
   int tiles, splits;
   long long rows, items; // queries of a head, work items
 };
 
-// natural log of 2^ref l
-__device__ __forceinline__ float log_sum(float ref, float l) {
+// natural log of a sum l against `top`
+template <int MODE> __device__ __forceinline__ float log_sum(const DenseGeo& q, float top, float l) {
   constexpr float kLn2Lo = 0.6931471805599453 - (double)kLn2;
-  return l > 0.f ? __builtin_fmaf(ref, kLn2, __builtin_fmaf(ref, kLn2Lo, logf(l))) : -INFINITY;
+  const Ref r = ref_of<MODE>(q, top);
+  return l > 0.f ? __builtin_fmaf(r.score, q.scale, __builtin_fmaf(r.x, kLn2, __builtin_fmaf(r.x, kLn2Lo, logf(l)))) : -INFINITY;
 }
 
 // NW waves, JW of which share their columns (1, or all)
@@ -65,14 +66,14 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
 
   Own<T, D> own[NQ];
   f32x16 z[NQ][D / 32];
-  float ref[NQ], sum[NQ];
+  float top[NQ], sum[NQ];
 #pragma unroll
   for (int h = 0; h < NQ; ++h) {
     own[h].load(g.Q + query_offset<MODE>(q, q.q, b, hd, min(first_row + 32 * h + (lane & 31), last_row)) * (long long)sizeof(T), hi);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) z[h][dt] = zero16();
     // below every finite score, so that scores of minus infinity weigh nothing from the start
-    ref[h] = -FLT_MAX;
+    top[h] = -FLT_MAX;
     sum[h] = 0.f;
   }
   const unsigned s_lane = scores_lane<T, D>(lane), m_lane = mix_lane<T, D>(lane);
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
       if (key0 >= len) break;
       f32x16 s[NQ];
       scores<T, D, NQ>(buf + sub * 32 * RB + s_lane, own, s);
-      float mx[NQ];
+      float mx[NQ], ref[NQ];
       bool moves = false;
       const int left = len - key0 - 8 * hi;
 #pragma unroll
@@ -121,15 +122,22 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
 #pragma unroll
         for (int a = 1; a < 16; ++a) m = fmaxf(m, s[h][a]);
         m = max_across_halves(m);
-        mx[h] = MODE == BIAS ? m : m * q.c2;
-        moves = moves || mx[h] - ref[h] > kLazy;
+        mx[h] = m;
+        ref[h] = MODE == BIAS ? top[h] : top[h] * q.c2;
+        moves = moves || (MODE == BIAS ? m - top[h] : (m - top[h]) * q.c2) > kLazy || (MODE != BIAS && fabsf(ref[h]) > kNear);
       }
-      if (__any(moves)) {
+      if (__any(moves)) {                              // (always, where a row is distant: its scores get their reference here)
 #pragma unroll
         for (int h = 0; h < NQ; ++h) {
-          const float to = fmaxf(ref[h], mx[h]), f = exp2_fast(ref[h] - to);
-          ref[h] = to;
+          const float to = fmaxf(top[h], mx[h]), f = moved<MODE>(q, top[h], to);
+          const Ref r = ref_of<MODE>(q, to);
+          top[h] = to;
+          ref[h] = r.x;
           sum[h] *= f;
+          if constexpr (MODE != BIAS) {
+#pragma unroll
+            for (int a = 0; a < 16; ++a) s[h][a] -= r.score;
+          }
 #pragma unroll
           for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -154,27 +162,27 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
     }
   }
   if constexpr (JW > 1) {
-    // the waves' references and sums, then their sums of P V against the largest reference
+    // the waves' tops and sums, then their sums of P V against the largest top
     float* buf = (float*)tiles;
     f32x2* stat = (f32x2*)(buf + NW * 32 * (D + 4));
     const float own_sum = sum_across_halves(sum[0]);
     tile_barrier();
-    if (hi == 0) stat[wave * 32 + lane] = f32x2{ref[0], own_sum};
+    if (hi == 0) stat[wave * 32 + lane] = f32x2{top[0], own_sum};
     tile_barrier();
-    float top = -FLT_MAX;
+    float most = -FLT_MAX;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, stat[w * 32 + (lane & 31)][0]);
-    join_waves<D, NW>(buf, wave, lane, z[0], exp2_fast(ref[0] - top), [&](int row, int c, f32x4 (&x)[2]) {
+    for (int w = 0; w < NW; ++w) most = fmaxf(most, stat[w * 32 + (lane & 31)][0]);
+    join_waves<D, NW>(buf, wave, lane, z[0], moved<MODE>(q, top[0], most), [&](int row, int c, f32x4 (&x)[2]) {
       const int rr = first_row + row;
       if (rr > last_row) return;
       float t = -FLT_MAX, l = 0.f;
 #pragma unroll
       for (int w = 0; w < NW; ++w) t = fmaxf(t, stat[w * 32 + row][0]);
 #pragma unroll
-      for (int w = 0; w < NW; ++w) l = __builtin_fmaf(stat[w * 32 + row][1], exp2_fast(stat[w * 32 + row][0] - t), l);
+      for (int w = 0; w < NW; ++w) l = __builtin_fmaf(stat[w * 32 + row][1], moved<MODE>(q, stat[w * 32 + row][0], t), l);
       if (g.splits == 1) {
         store8<T>(g.O + (query_offset<MODE>(q, q.o, b, hd, rr) + c) * (long long)sizeof(T), x, l > 0.f ? 1.f / l : 0.f);
-        if (g.lse && c == 0) g.lse[bh * g.rows + rr] = log_sum(t, l);
+        if (g.lse && c == 0) g.lse[bh * g.rows + rr] = log_sum<MODE>(q, t, l);
       } else {
         const long long at = item * RT + row;
         store8<float>((unsigned char*)(g.part + at * D + c), x, 1.f);
@@ -191,11 +199,11 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
     if (g.splits == 1) {
       const int rc = min(rr, last_row);
       store_column<T, D>(g.O + query_offset<MODE>(q, q.o, b, hd, rc) * (long long)sizeof(T), hi, z[h], l > 0.f ? 1.f / l : 0.f, there);
-      if (g.lse && there && hi == 0) g.lse[bh * g.rows + rr] = log_sum(ref[h], l);
+      if (g.lse && there && hi == 0) g.lse[bh * g.rows + rr] = log_sum<MODE>(q, top[h], l);
     } else {
       const long long at = item * RT + wave * (32 * NQ) + 32 * h + (lane & 31);
       store_column<float, D>((unsigned char*)(g.part + at * D), hi, z[h], 1.f, there);
-      if (there && hi == 0) *(f32x2*)(g.part + g.items * RT * D + at * 2) = f32x2{ref[h], l};
+      if (there && hi == 0) *(f32x2*)(g.part + g.items * RT * D + at * 2) = f32x2{top[h], l};
     }
   }
 }
@@ -218,13 +226,13 @@ __global__ __launch_bounds__(256) void dense_join_kernel(DenseGeo q, FwdArgs g, 
   float top = -FLT_MAX, l = 0.f;
   for (int s = lane; s < g.splits; s += 64) {
     const f32x2 x = *(const f32x2*)(stat + (long long)s * RT * 2);
-    if (x[1] > 0.f) top = fmaxf(top, x[0]);
+    top = fmaxf(top, x[0]);            // (of a piece without keys: -FLT_MAX, with sums of 0)
   }
 #pragma unroll
   for (int i = 32; i >= 1; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
   for (int s = lane; s < g.splits; s += 64) {
     const f32x2 x = *(const f32x2*)(stat + (long long)s * RT * 2);
-    if (x[1] > 0.f) l = __builtin_fmaf(x[1], exp2_fast(x[0] - top), l);
+    l = __builtin_fmaf(x[1], moved<MODE>(q, x[0], top), l);
   }
 #pragma unroll
   for (int i = 32; i >= 1; i >>= 1) l += __shfl_xor(l, i);
@@ -233,7 +241,7 @@ __global__ __launch_bounds__(256) void dense_join_kernel(DenseGeo q, FwdArgs g, 
 #pragma unroll 8
   for (int s = w; s < g.splits; s += W) {
     const f32x2 x = *(const f32x2*)(stat + (long long)s * RT * 2);
-    const float f = x[1] > 0.f ? exp2_fast(x[0] - top) : 0.f;
+    const float f = moved<MODE>(q, x[0], top);
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(part[(long long)s * RT * D + lane * E + e], f, o[e]);
   }
@@ -251,7 +259,7 @@ __global__ __launch_bounds__(256) void dense_join_kernel(DenseGeo q, FwdArgs g, 
   T* out = (T*)g.O + query_offset<MODE>(q, q.o, b, hd, rr);
 #pragma unroll
   for (int e = 0; e < E; ++e) out[lane * E + e] = (T)(l > 0.f ? o[e] / l : 0.f);
-  if (g.lse && lane == 0) g.lse[row] = log_sum(top, l);
+  if (g.lse && lane == 0) g.lse[row] = log_sum<MODE>(q, top, l);
 }
 
 }  // namespace dense

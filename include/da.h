@@ -294,6 +294,8 @@ int da_forward_global(const da_problem* p, const void* Q, const void* K, const v
  *     x_ij = scale q_i.k_j (+ the bias of da_bias_attn)    lse_i = log sum_j exp x_ij    o_i = sum_j exp(x_ij - lse_i) v_j
  * A key whose x is minus infinity weighs nothing; a row with nothing to attend (n_b = 0, or minus infinity throughout) has o = 0
  * and lse = -inf, and its gradients are 0.
+ * Scores of any finite size: a row's probabilities add up to 1 in both directions.  (Backward, rows with |lse| above 1024 in bf16 or 128 in
+ * float32, more than a float holds log(sum) beside, take one more pass over the keys.)
  * K and V rows at or behind n_b are not read (they may hold anything) and get zero rows of dK and dV; kv_len outside [0, M] is
  * brought into it.
  */

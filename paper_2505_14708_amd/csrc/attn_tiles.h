@@ -328,8 +328,8 @@ __device__ __forceinline__ void fill_bias(float* lds, const RelRule& rule, const
   const int n = bias_entries(rule.cut);
   for (int i = thread; i < n; i += threads) {
     const float b = (float)table[(long long)rel_bucket(rule, i - rule.cut - kBiasPad) * H + h];
-    // A mask of the type's lowest value is minus infinity here: beside numbers of that size a score leaves no trace, nor does log(sum) in
-    // lse, from which the backward pass could not make the probabilities again.
+    // A mask of the type's lowest value is minus infinity here: a row that only such entries reach has nothing to attend, and with a score
+    // added they could be minus infinity or not.
     lds[i] = b <= kMasks ? -INFINITY : b * kLog2e;
   }
 }

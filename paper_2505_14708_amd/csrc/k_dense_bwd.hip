@@ -28,6 +28,7 @@ struct BwdArgs {
   unsigned char *dQ, *dK, *dV;
   void* dtable;
   float *start, *delta;            // [heads][padded rows]: where a row's scores start (start_of), -delta
+  float *top, *log_l;              // the same: of rows in a far tile (kFarLse) the largest score and log2(sum) against it
   float *dq_part, *r_part, *dkv_part;  // sums of pieces: dQ, rows of ds, dK and dV
   float* bias_part;                // [work item][buckets]
   long long rows, padded;          // rows of a head as the kernels see them, and rounded up to 32
@@ -96,7 +97,59 @@ __device__ __forceinline__ void bucket_range(const RelRule& t, int c, int& first
 // What is added to a row's scores in the second kernel.  bf16: the sums of the matrix product start from -lse / scale, which costs nothing.
 // float32: subtracted at the end, -lse log2(e) (from the start it would add its own roundings, of the size of lse, to every step's).
 // Minus infinity where a row has nothing to attend or is padding: p is 0.
-template <class T> __device__ __forceinline__ float start_of(const DenseGeo& q, float lse2) { return sizeof(T) == 2 ? -lse2 / q.c2 : -lse2; }
+template <class T> __device__ __forceinline__ float start_of(const DenseGeo& q, float lse2) {
+  const float x = sizeof(T) == 2 ? -lse2 / q.c2 : -lse2;
+  return fabsf(x) < FLT_MIN ? 0.f : x;
+}
+
+// lse holds log(sum) beside the largest score in one float.  What it was rounded by, and its product with log2(e), scale all probabilities of a row by
+// 1 +- |lse| 2^-23.6 (a single score is known no better, but they would no longer add up to 1): beside the operands' rounding that is small up to kFarLse
+// (bfloat16: 8e-5 of 2e-3; float32: 1e-5, as its scores' own), and from 2^24 on it is everything.  So a workgroup with a row beyond makes its
+// rows' largest scores and sums again, in a round of its own ahead of the others, takes the probabilities from those, and leaves them for the second
+// kernel, with a mark in `start`.  (The mark is no ordinary row's start, and nothing beside a score where sums start from it.)
+template <class T> constexpr float kFarLse = sizeof(T) == 2 ? 1024.f : 128.f;
+constexpr int kFarMark = 1;
+template <class T> __device__ __forceinline__ bool is_far_lse(float l) { return fabsf(l) > kFarLse<T> && l > -FLT_MAX; }
+
+// The largest x (with a bias) or score (without) of each of the wave's 32 queries among all keys, and the sum of exp2(x - that), of waves that share
+// their queries a wave's part of both; through the first tile's memory, one tile at a time.
+template <class T, int D, int NW, int JW, int MODE>
+__device__ __forceinline__ void far_sums(const DenseGeo& q, const Own<T, D> (&own)[1], const unsigned char* kb, long long ks, int len, int n_tiles,
+                                         unsigned lds, unsigned s_lane, int wave, int lane, const float* bias_row, int first_row, int last_row,
+                                         float& top, float& sum) {
+  constexpr int KB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>;
+  const int hi = lane >> 5;
+  top = -FLT_MAX;
+  sum = 0.f;
+  for (int t = 0; t < n_tiles; ++t) {
+    tile_barrier();
+    load_tile<T, D, KB, NW>(kb, ks, t * KB, len - 1, lds, wave);
+    wait_loads();
+    tile_barrier();
+    if (first_row > last_row) continue;
+    for (int i = 0; i < KB / 32 / JW; ++i) {
+      const int sub = JW > 1 ? wave : i, key0 = t * KB + 32 * sub;
+      if (key0 >= len) break;
+      f32x16 s[1];
+      scores<T, D, 1>(lds + sub * 32 * RB + s_lane, own, s);
+      const int left = len - key0 - 8 * hi, low = MODE == BIAS ? key0 - first_row - q.q_pos : 0, wide = MODE == BIAS ? q.rule.cut + kBiasPad : 0;
+      float m = -FLT_MAX;
+#pragma unroll
+      for (int a = 0; a < 16; ++a) {
+        const int r = 16 * (a >> 3) + (a & 7);
+        if constexpr (MODE == BIAS) s[0][a] = biased<T>(q, s[0][a], bias_row[min(max(low + 8 * hi + r - (lane & 31) + wide, 0), 2 * wide)]);
+        s[0][a] = r < left ? s[0][a] : -INFINITY;
+        m = fmaxf(m, s[0][a]);
+      }
+      m = fmaxf(top, max_across_halves(m));
+      sum *= exp2_fast(MODE == BIAS ? top - m : (top - m) * q.c2);
+#pragma unroll
+      for (int a = 0; a < 16; ++a) sum += MODE == BIAS ? exp2_fast(s[0][a] - m) : power_of<T>(q, s[0][a] - m, 0.f);
+      top = m;
+    }
+  }
+  sum = sum_across_halves(sum);
+}
 
 template <class T, int D, int JW> constexpr int kDqWaves = JW > 1 || kRowBytes<T, D> > 256 ? 1 : 2;
 
@@ -144,7 +197,11 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
     delta = sum_across_halves(delta);
   }
   const float l = g.lse[bh * g.rows + rc];
-  const float lse2 = rr <= last_row && l != -INFINITY ? l * kLog2e : INFINITY;
+  float lse2 = rr <= last_row && l != -INFINITY ? l * kLog2e : INFINITY;   // far: log2(sum)
+  bool far = false;                // the same for all waves of the workgroup
+#pragma unroll
+  for (int i = 0; i < RT; i += 64) far = far || is_far_lse<T>(g.lse[bh * g.rows + min(tile * RT + i + lane % (RT < 64 ? RT : 64), last_row)]);
+  far = __builtin_amdgcn_readfirstlane(__any(far));
   float off = 0.f;                 // this lane's part of the row's sum of ds
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) z[0][dt] = zero16();
@@ -155,6 +212,34 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
   // (dQ's error in norm with 4 to 31 keys 2.5e-3 to 3.8e-3 without, the roundings of ds and dQ 2.4e-3.  Over many keys what delta is off by
   // hardly shows.)
   const bool exact = g.splits == 1 && n_tiles <= 2;
+  float top = 0.f;
+  if (far) {
+    wait_loads();
+    float sum;
+    far_sums<T, D, NW, JW, MODE>(q, own, kb, ks, len, n_tiles, lds, s_lane, wave, lane, bias_row, first_row, last_row, top, sum);
+    if constexpr (JW > 1) {
+      if (hi == 0) parts[wave * 32 + lane] = top;
+      __syncthreads();
+      float most = -FLT_MAX;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) most = fmaxf(most, parts[w * 32 + (lane & 31)]);
+      sum *= exp2_fast(MODE == BIAS ? top - most : (top - most) * q.c2);
+      __syncthreads();
+      if (hi == 0) parts[wave * 32 + lane] = sum;
+      __syncthreads();
+      sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) sum += parts[w * 32 + (lane & 31)];
+      __syncthreads();
+      top = most;
+    }
+    lse2 = rr <= last_row && sum > 0.f ? __builtin_log2f(sum) : INFINITY;
+    tile_barrier();
+    if (t0 < t1) {
+      load_tile<T, D, KB, NW>(kb, ks, t0 * KB, len - 1, lds, wave);
+      load_tile<T, D, KB, NW>(vb, vs, t0 * KB, len - 1, lds + TILE, wave);
+    }
+  }
   for (int round = exact ? 0 : 1; round < 2; ++round) {
     for (int t = t0; t < t1; ++t) {
       const unsigned buf = lds + ((t - t0) & 1) * (2 * TILE);
@@ -177,16 +262,30 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
         if constexpr (MODE == BIAS) {
           const int low = key0 - first_row - q.q_pos;          // r of key 0 and query 0 of the square
           if (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut) {
-            const float far = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0] - lse2;
+            const float out = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
+            if (far) {
 #pragma unroll
-            for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], far);
+              for (int a = 0; a < 16; ++a) s[0][a] = exp2_fast((biased<T>(q, s[0][a], out) - top) - lse2);
+            } else {
+#pragma unroll
+              for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], out - lse2);
+            }
           } else {
             f32x16 bs;
             read_bias<1>(bias_lds + 4 * (low + 8 * hi - (lane & 31) + q.rule.cut + kBiasPad), bs);
+            if (far) {
 #pragma unroll
-            for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], bs[a] - lse2);
+              for (int a = 0; a < 16; ++a) s[0][a] = exp2_fast((biased<T>(q, s[0][a], bs[a]) - top) - lse2);
+            } else {
+#pragma unroll
+              for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], bs[a] - lse2);
+            }
           }
         } else {
+          if (far) {
+#pragma unroll
+            for (int a = 0; a < 16; ++a) s[0][a] -= top;
+          }
 #pragma unroll
           for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], -lse2);
         }
@@ -242,8 +341,28 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
     if (there && hi == 0) g.r_part[at] = off;
   }
   if (split == 0 && hi == 0 && rr < g.padded) {
-    g.start[bh * g.padded + rr] = start_of<T>(q, lse2);
+    g.start[bh * g.padded + rr] = far ? __int_as_float(kFarMark) : start_of<T>(q, lse2);
+    if (far) {
+      g.top[bh * g.padded + rr] = top;
+      g.log_l[bh * g.padded + rr] = lse2;
+    }
     g.delta[bh * g.padded + rr] = there ? -(g.splits == 1 ? delta + off : delta) : 0.f;
+  }
+}
+
+// Probabilities of a square (keys on the lanes) whose queries are in a far tile: rows r of top and log_l for the registers of row r.  (None is above 1:
+// the scores are sums in another order here.)  r0: key - query of the lane's key and the square's row 8 (l / 32).
+template <class T, int MODE>
+__device__ __forceinline__ void far_powers(const DenseGeo& q, f32x16& s, const float* top, const float* log_l, const float* bias_row, int r0) {
+  const int wide = MODE == BIAS ? q.rule.cut + kBiasPad : 0;
+#pragma unroll
+  for (int a = 0; a < 16; ++a) {
+    const int r = 16 * (a >> 3) + (a & 7);
+    float x;
+    if constexpr (MODE == BIAS) x = biased<T>(q, s[a], bias_row[min(max(r0 - r + wide, 0), 2 * wide)]) - top[r];
+    else x = biased<T>(q, s[a] - top[r], 0.f);
+    s[a] = exp2_fast(fminf(x, 0.f) - log_l[r]);
+    if (a % 4 == 3) __builtin_amdgcn_sched_barrier(0);            // (a few rows' numbers at a time: registers)
   }
 }
 
@@ -348,6 +467,7 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
       // Sums start from what belongs to their rows (start_of, -delta): registers 4i .. 4i + 3 have rows 16(i / 2) + 8 hi + 4(i % 2) + 0..3.
       constexpr bool kLate = sizeof(T) == 4;
       f32x16 s[1], dp[1], late;
+      int mark = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const unsigned at = buf + 2 * TILE + 4 * (32 * sub + 16 * (i >> 1) + 8 * hi + 4 * (i & 1));
@@ -358,13 +478,16 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
           s[0][4 * i + e] = kLate ? 0.f : l[e];
           dp[0][4 * i + e] = dl[e];
         }
+        if (i == 0) mark = __builtin_amdgcn_readfirstlane(__float_as_int(l[0]));
       }
       add_scores<T, D, 1>(buf + sub * 32 * RB + s_lane, own_k, s);
       if constexpr (V_IN_LDS) add_scores_lds<D>(buf + TILE + sub * 32 * RB + s_lane, lds + 2 * STAGE + wave * 32 * RB + lane * 16, dp[0]);
       else add_scores<T, D, 1>(buf + TILE + sub * 32 * RB + s_lane, own_v, dp);
       const int low = MODE == BIAS ? key0 - row0 - q.q_pos : 0;      // r of key 0 and query 0 of the square
       const bool is_far = MODE == BIAS && (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut);
-      if constexpr (MODE == BIAS) {
+      if (mark == kFarMark) {
+        far_powers<T, MODE>(q, s[0], g.top + stat + row0 + 8 * hi, g.log_l + stat + row0 + 8 * hi, bias_row, low + (lane & 31) - 8 * hi);
+      } else if constexpr (MODE == BIAS) {
         if (is_far) {
           const float far = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
 #pragma unroll
@@ -546,7 +669,7 @@ constexpr size_t kLds = 160 * 1024;
 struct BwdPlan {
   int join, row_tile, tiles, splits;                                            // dq
   int kv_join, kv_tiles, kv_splits, per_head, row_tiles, q_tile;                // dkv
-  size_t start, delta, dq_part, r_part, dkv_part, bias_part, total;
+  size_t start, delta, top, log_l, dq_part, r_part, dkv_part, bias_part, total;
 };
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -599,6 +722,8 @@ BwdPlan plan_bwd(const DenseGeo& q) {
   size_t off = 0;
   p.start = off; off += align_up(heads * padded * sizeof(float));
   p.delta = off; off += align_up(heads * padded * sizeof(float));
+  p.top = off; off += align_up(heads * padded * sizeof(float));
+  p.log_l = off; off += align_up(heads * padded * sizeof(float));
   p.dq_part = off; off += p.splits > 1 ? align_up((size_t)heads * p.tiles * p.splits * p.row_tile * q.d * sizeof(float)) : 0;
   p.r_part = off; off += p.splits > 1 ? align_up((size_t)heads * p.tiles * p.splits * p.row_tile * sizeof(float)) : 0;
   p.dkv_part = off; off += p.kv_splits > 1 ? align_up(2 * (size_t)p.kv_splits * kv_heads * q.M * q.d * sizeof(float)) : 0;
@@ -660,6 +785,7 @@ hipError_t launch_dense_bwd(const DenseGeo& q, const void* Q, const void* K, con
   a.dQ = (unsigned char*)dQ; a.dK = (unsigned char*)dK; a.dV = (unsigned char*)dV; a.dtable = dtable;
   char* base = (char*)ws;
   a.start = (float*)(base + p.start); a.delta = (float*)(base + p.delta);
+  a.top = (float*)(base + p.top); a.log_l = (float*)(base + p.log_l);
   a.dq_part = (float*)(base + p.dq_part); a.r_part = (float*)(base + p.r_part); a.dkv_part = (float*)(base + p.dkv_part);
   a.bias_part = (float*)(base + p.bias_part);
   a.rows = dense_rows(q);

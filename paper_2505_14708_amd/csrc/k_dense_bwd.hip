@@ -177,13 +177,18 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
   const unsigned char* kb = g.K + (b * q.k.sb + hk * q.k.sh) * (long long)sizeof(T);
   const unsigned char* vb = g.V + (b * q.v.sb + hk * q.v.sh) * (long long)sizeof(T);
   const unsigned lds = (unsigned)(uintptr_t)(lds_f32*)tiles;
+  const int rr = first_row + (lane & 31), rc = min(rr, last_row);
+  // lse of the wave's and of all of the workgroup's rows, ahead of the longer loads
+  const float l = g.lse[bh * g.rows + rc];
+  float all_l[RT > 64 ? RT / 64 : 1];
+#pragma unroll
+  for (int i = 0; i < RT; i += 64) all_l[i / 64] = g.lse[bh * g.rows + min(tile * RT + i + lane % (RT < 64 ? RT : 64), last_row)];
   if (t0 < t1) {
     load_tile<T, D, KB, NW>(kb, ks, t0 * KB, len - 1, lds, wave);
     load_tile<T, D, KB, NW>(vb, vs, t0 * KB, len - 1, lds + TILE, wave);
   }
   if constexpr (MODE == BIAS) fill_bias<T>(bias_row, q.rule, (const T*)g.table, q.H, hd, threadIdx.x, 64 * NW);
 
-  const int rr = first_row + (lane & 31), rc = min(rr, last_row);
   Own<T, D> own[1], grad[1];
   f32x16 z[1][D / 32];
   own[0].load(g.Q + query_offset<MODE>(q, q.q, b, hd, rc) * (long long)sizeof(T), hi);
@@ -196,11 +201,9 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
     for (int t = 0; t < Own<T, D>::N; ++t) delta = dot_piece<T>(grad[0].x[t], out.x[t], delta);
     delta = sum_across_halves(delta);
   }
-  const float l = g.lse[bh * g.rows + rc];
   float lse2 = rr <= last_row && l != -INFINITY ? l * kLog2e : INFINITY;   // far: log2(sum)
   bool far = false;                // the same for all waves of the workgroup
-#pragma unroll
-  for (int i = 0; i < RT; i += 64) far = far || is_far_lse<T>(g.lse[bh * g.rows + min(tile * RT + i + lane % (RT < 64 ? RT : 64), last_row)]);
+  for (float x : all_l) far = far || is_far_lse<T>(x);
   far = __builtin_amdgcn_readfirstlane(__any(far));
   float off = 0.f;                 // this lane's part of the row's sum of ds
 #pragma unroll
@@ -213,7 +216,7 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
   // hardly shows.)
   const bool exact = g.splits == 1 && n_tiles <= 2;
   float top = 0.f;
-  if (far) {
+  if (__builtin_expect(far, 0)) {
     wait_loads();
     float sum;
     far_sums<T, D, NW, JW, MODE>(q, own, kb, ks, len, n_tiles, lds, s_lane, wave, lane, bias_row, first_row, last_row, top, sum);
@@ -259,11 +262,12 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
         f32x16 s[1], dp[1];
         scores<T, D, 1>(buf + sub * 32 * RB + s_lane, own, s);
         scores<T, D, 1>(buf + TILE + sub * 32 * RB + s_lane, grad, dp);
+        const int left = len - key0 - 8 * hi;
         if constexpr (MODE == BIAS) {
           const int low = key0 - first_row - q.q_pos;          // r of key 0 and query 0 of the square
           if (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut) {
             const float out = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
-            if (far) {
+            if (__builtin_expect(far, 0)) {
 #pragma unroll
               for (int a = 0; a < 16; ++a) s[0][a] = exp2_fast((biased<T>(q, s[0][a], out) - top) - lse2);
             } else {
@@ -273,7 +277,7 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
           } else {
             f32x16 bs;
             read_bias<1>(bias_lds + 4 * (low + 8 * hi - (lane & 31) + q.rule.cut + kBiasPad), bs);
-            if (far) {
+            if (__builtin_expect(far, 0)) {
 #pragma unroll
               for (int a = 0; a < 16; ++a) s[0][a] = exp2_fast((biased<T>(q, s[0][a], bs[a]) - top) - lse2);
             } else {
@@ -282,15 +286,14 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
             }
           }
         } else {
-          if (far) {
+          if (far || key0 + 32 > len) {
 #pragma unroll
-            for (int a = 0; a < 16; ++a) s[0][a] -= top;
+            for (int a = 0; a < 16; ++a) s[0][a] = 16 * (a >> 3) + (a & 7) < left ? s[0][a] - top : -INFINITY;
           }
 #pragma unroll
           for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], -lse2);
         }
-        if (key0 + 32 > len) {
-          const int left = len - key0 - 8 * hi;
+        if (MODE == BIAS && key0 + 32 > len) {
 #pragma unroll
           for (int a = 0; a < 16; ++a) s[0][a] = 16 * (a >> 3) + (a & 7) < left ? s[0][a] : 0.f;
         }
@@ -342,7 +345,7 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
   }
   if (split == 0 && hi == 0 && rr < g.padded) {
     g.start[bh * g.padded + rr] = far ? __int_as_float(kFarMark) : start_of<T>(q, lse2);
-    if (far) {
+    if (__builtin_expect(far, 0)) {
       g.top[bh * g.padded + rr] = top;
       g.log_l[bh * g.padded + rr] = lse2;
     }
@@ -485,7 +488,7 @@ __global__ __launch_bounds__(64 * NW, (kDkvWaves<T, D, JW>)) void dense_dkv_kern
       else add_scores<T, D, 1>(buf + TILE + sub * 32 * RB + s_lane, own_v, dp);
       const int low = MODE == BIAS ? key0 - row0 - q.q_pos : 0;      // r of key 0 and query 0 of the square
       const bool is_far = MODE == BIAS && (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut);
-      if (mark == kFarMark) {
+      if (__builtin_expect(mark == kFarMark, 0)) {
         far_powers<T, MODE>(q, s[0], g.top + stat + row0 + 8 * hi, g.log_l + stat + row0 + 8 * hi, bias_row, low + (lane & 31) - 8 * hi);
       } else if constexpr (MODE == BIAS) {
         if (is_far) {

@@ -37,6 +37,9 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
   static_assert(JW == 1 || (JW == NW && NQ == 1), "one set of columns to join");
   constexpr int KB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * NQ * (NW / JW);
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * TILE];   // K, V, K, V
+  // Each lane's tops (ref_of), which only a reference that moves asks for.  (In registers they would be two more than two sets of 128 channels have:
+  // 40 heads of 75600 by 512 983 us instead of 925, and 916 without rows of distant scores; made anew from `ref` or compared each time 2 % more.)
+  __shared__ float tops[NQ][MODE == BIAS ? 1 : 64 * NW];
   extern __shared__ __attribute__((aligned(16))) float bias_row[];
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
   if (id >= g.items) return;
@@ -66,18 +69,22 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
 
   Own<T, D> own[NQ];
   f32x16 z[NQ][D / 32];
-  float top[NQ], sum[NQ];
+  float ref[NQ], sum[NQ];                              // ref: Ref's x
 #pragma unroll
   for (int h = 0; h < NQ; ++h) {
     own[h].load(g.Q + query_offset<MODE>(q, q.q, b, hd, min(first_row + 32 * h + (lane & 31), last_row)) * (long long)sizeof(T), hi);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) z[h][dt] = zero16();
     // below every finite score, so that scores of minus infinity weigh nothing from the start
-    top[h] = -FLT_MAX;
+    ref[h] = -FLT_MAX;
+    if constexpr (MODE != BIAS) tops[h][threadIdx.x] = -FLT_MAX;
     sum[h] = 0.f;
   }
   const unsigned s_lane = scores_lane<T, D>(lane), m_lane = mix_lane<T, D>(lane);
   const unsigned bias_lds = MODE == BIAS ? (unsigned)(uintptr_t)(lds_f32*)bias_row : 0u;
+
+  unsigned long long distant = 0;                      // lanes with a distant row
+  auto top_of = [&](int h) { return MODE == BIAS ? ref[h] : tops[h][threadIdx.x]; };
 
   for (int t = t0; t < t1; ++t) {
     const unsigned buf = lds + ((t - t0) & 1) * (2 * TILE);
@@ -96,7 +103,7 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
       if (key0 >= len) break;
       f32x16 s[NQ];
       scores<T, D, NQ>(buf + sub * 32 * RB + s_lane, own, s);
-      float mx[NQ], ref[NQ];
+      float mx[NQ];
       bool moves = false;
       const int left = len - key0 - 8 * hi;
 #pragma unroll
@@ -123,16 +130,17 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
         for (int a = 1; a < 16; ++a) m = fmaxf(m, s[h][a]);
         m = max_across_halves(m);
         mx[h] = m;
-        ref[h] = MODE == BIAS ? top[h] : top[h] * q.c2;
-        moves = moves || (MODE == BIAS ? m - top[h] : (m - top[h]) * q.c2) > kLazy || (MODE != BIAS && fabsf(ref[h]) > kNear);
+        moves = moves || (MODE == BIAS ? m : m * q.c2) - ref[h] > kLazy;
       }
-      if (__any(moves)) {                              // (always, where a row is distant: its scores get their reference here)
+      if (__builtin_amdgcn_ballot_w64(moves) | distant) {     // (a distant row's differences are taken here)
+        bool any = false;
 #pragma unroll
         for (int h = 0; h < NQ; ++h) {
-          const float to = fmaxf(top[h], mx[h]), f = moved<MODE>(q, top[h], to);
+          const float top = top_of(h), to = fmaxf(top, mx[h]), f = moved<MODE>(q, top, to);
           const Ref r = ref_of<MODE>(q, to);
-          top[h] = to;
+          if constexpr (MODE != BIAS) tops[h][threadIdx.x] = to;
           ref[h] = r.x;
+          any = any || is_distant<MODE>(q, to);
           sum[h] *= f;
           if constexpr (MODE != BIAS) {
 #pragma unroll
@@ -143,6 +151,7 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
 #pragma unroll
             for (int a = 0; a < 16; ++a) z[h][dt][a] *= f;
         }
+        distant = __builtin_amdgcn_ballot_w64(any);
       }
 #pragma unroll
       for (int h = 0; h < NQ; ++h) {
@@ -167,12 +176,12 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
     f32x2* stat = (f32x2*)(buf + NW * 32 * (D + 4));
     const float own_sum = sum_across_halves(sum[0]);
     tile_barrier();
-    if (hi == 0) stat[wave * 32 + lane] = f32x2{top[0], own_sum};
+    if (hi == 0) stat[wave * 32 + lane] = f32x2{top_of(0), own_sum};
     tile_barrier();
     float most = -FLT_MAX;
 #pragma unroll
     for (int w = 0; w < NW; ++w) most = fmaxf(most, stat[w * 32 + (lane & 31)][0]);
-    join_waves<D, NW>(buf, wave, lane, z[0], moved<MODE>(q, top[0], most), [&](int row, int c, f32x4 (&x)[2]) {
+    join_waves<D, NW>(buf, wave, lane, z[0], moved<MODE>(q, top_of(0), most), [&](int row, int c, f32x4 (&x)[2]) {
       const int rr = first_row + row;
       if (rr > last_row) return;
       float t = -FLT_MAX, l = 0.f;
@@ -199,11 +208,11 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
     if (g.splits == 1) {
       const int rc = min(rr, last_row);
       store_column<T, D>(g.O + query_offset<MODE>(q, q.o, b, hd, rc) * (long long)sizeof(T), hi, z[h], l > 0.f ? 1.f / l : 0.f, there);
-      if (g.lse && there && hi == 0) g.lse[bh * g.rows + rr] = log_sum<MODE>(q, top[h], l);
+      if (g.lse && there && hi == 0) g.lse[bh * g.rows + rr] = log_sum<MODE>(q, top_of(h), l);
     } else {
       const long long at = item * RT + wave * (32 * NQ) + 32 * h + (lane & 31);
       store_column<float, D>((unsigned char*)(g.part + at * D), hi, z[h], 1.f, there);
-      if (there && hi == 0) *(f32x2*)(g.part + g.items * RT * D + at * 2) = f32x2{top[h], l};
+      if (there && hi == 0) *(f32x2*)(g.part + g.items * RT * D + at * 2) = f32x2{top_of(h), l};
     }
   }
 }

@@ -37,9 +37,6 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
   static_assert(JW == 1 || (JW == NW && NQ == 1), "one set of columns to join");
   constexpr int KB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * NQ * (NW / JW);
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * TILE];   // K, V, K, V
-  // Each lane's tops (ref_of), which only a reference that moves asks for.  (In registers they would be two more than two sets of 128 channels have:
-  // 40 heads of 75600 by 512 983 us instead of 925, and 916 without rows of distant scores; made anew from `ref` or compared each time 2 % more.)
-  __shared__ float tops[NQ][MODE == BIAS ? 1 : 64 * NW];
   extern __shared__ __attribute__((aligned(16))) float bias_row[];
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
   if (id >= g.items) return;
@@ -69,22 +66,21 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
 
   Own<T, D> own[NQ];
   f32x16 z[NQ][D / 32];
-  float ref[NQ], sum[NQ];                              // ref: Ref's x
+  float ref[NQ], top[NQ], sum[NQ];                     // ref: Ref's x of top, with a bias the top itself
 #pragma unroll
   for (int h = 0; h < NQ; ++h) {
     own[h].load(g.Q + query_offset<MODE>(q, q.q, b, hd, min(first_row + 32 * h + (lane & 31), last_row)) * (long long)sizeof(T), hi);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) z[h][dt] = zero16();
     // below every finite score, so that scores of minus infinity weigh nothing from the start
-    ref[h] = -FLT_MAX;
-    if constexpr (MODE != BIAS) tops[h][threadIdx.x] = -FLT_MAX;
+    ref[h] = top[h] = -FLT_MAX;
     sum[h] = 0.f;
   }
   const unsigned s_lane = scores_lane<T, D>(lane), m_lane = mix_lane<T, D>(lane);
   const unsigned bias_lds = MODE == BIAS ? (unsigned)(uintptr_t)(lds_f32*)bias_row : 0u;
 
+  auto top_of = [&](int h) { return MODE == BIAS ? ref[h] : top[h]; };
   unsigned long long distant = 0;                      // lanes with a distant row
-  auto top_of = [&](int h) { return MODE == BIAS ? ref[h] : tops[h][threadIdx.x]; };
 
   for (int t = t0; t < t1; ++t) {
     const unsigned buf = lds + ((t - t0) & 1) * (2 * TILE);
@@ -132,26 +128,30 @@ __global__ __launch_bounds__(64 * NW, JW > 1 ? 1 : 2) void dense_fwd_kernel(Dens
         mx[h] = m;
         moves = moves || (MODE == BIAS ? m : m * q.c2) - ref[h] > kLazy;
       }
-      if (__builtin_amdgcn_ballot_w64(moves) | distant) {     // (a distant row's differences are taken here)
+      if (__builtin_amdgcn_ballot_w64(moves) | distant) {     // (a distant row: its differences are taken in here)
         bool any = false;
+        float score[NQ];
 #pragma unroll
         for (int h = 0; h < NQ; ++h) {
-          const float top = top_of(h), to = fmaxf(top, mx[h]), f = moved<MODE>(q, top, to);
+          const float to = fmaxf(top_of(h), mx[h]), f = moved<MODE>(q, top_of(h), to);
           const Ref r = ref_of<MODE>(q, to);
-          if constexpr (MODE != BIAS) tops[h][threadIdx.x] = to;
+          top[h] = to;
           ref[h] = r.x;
           any = any || is_distant<MODE>(q, to);
           sum[h] *= f;
-          if constexpr (MODE != BIAS) {
-#pragma unroll
-            for (int a = 0; a < 16; ++a) s[h][a] -= r.score;
-          }
+          score[h] = r.score;
 #pragma unroll
           for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
             for (int a = 0; a < 16; ++a) z[h][dt][a] *= f;
         }
         distant = __builtin_amdgcn_ballot_w64(any);
+        if (distant) {
+#pragma unroll
+          for (int h = 0; h < NQ; ++h)
+#pragma unroll
+            for (int a = 0; a < 16; ++a) s[h][a] -= score[h];
+        }
       }
 #pragma unroll
       for (int h = 0; h < NQ; ++h) {

@@ -684,7 +684,12 @@ inline size_t dkv_bias_lds(const DenseGeo& q, int waves) {
   return (n + 2 * waves * n) * sizeof(float);
 }
 
-// Workgroups of four waves with 32 queries (keys) each, or, where they are too few, of waves that share 32 and take the other side in turn.
+// Workgroups of four waves with 32 queries (keys) each, or, where they are too few, of waves that share 32 and take the other side in turn.  Either is cut
+// where that fills its rounds.  The waves also join where there are many workgroups but three of the four waves would have nothing, if the other side is
+// four of their tiles or more (960 heads of 32 by 32, 128 channels: 29 us, joining 65).  Not in bfloat16 with 128 channels, where two workgroups
+// fit a CU and one that joins (960 heads of 513 queries by 16 keys: 180 us, joining 196).
+// 192 heads of 32760 queries by 16 keys, 128 channels, bfloat16: 2602 us uncut with one wave of four at work, 1951 in 8 pieces, 1948 in 4 joining; float32,
+// 8190 queries: 3232, 2731 and 2032.  By 64 keys: 2765, 2221 and 2464; 3699, 3220 and 3363.
 BwdPlan plan_bwd(const DenseGeo& q) {
   BwdPlan p;
   const long long rows = dense_rows(q), heads = (long long)q.B * dense_heads(q), kv_heads = (long long)q.B * q.Hk;
@@ -692,29 +697,33 @@ BwdPlan plan_bwd(const DenseGeo& q) {
   const int row_bytes = q.d * (f32 ? 4 : 2), tile = row_bytes > 256 ? 32 : 64, enough = kCUs / 4 * 3;
   const int kv_tile = !f32 && q.d == 128 && q.bias ? 32 : tile;
   const int joined = row_bytes > 256 ? 64 : 128, join_slots = row_bytes == 128 ? 2 * kCUs : kCUs;      // rows of a joining workgroup's tile
+  const int few = f32 || q.d == 64 ? 32 : 0;
   const int slots = row_bytes > 256 ? kCUs : 2 * kCUs;                                                 // (one wave to a SIMD there)
-  auto pieces_joined = [&](long long wgs, long long units) {
+  auto pieces_joined = [&](long long wgs, long long units, double join_mb) {
+    if (2 * wgs > join_slots) return cut(wgs, units, join_slots, 2 * product_us(q), join_mb);
     long long n = join_slots / wgs;
     n = n > units / 2 ? units / 2 : n;
     return (int)(n < 1 ? 1 : n);
   };
   long long wgs = heads * ((rows + 127) / 128);
   p.join = 0;
-  p.splits = rows > 64 ? cut(wgs, (q.M + tile - 1) / tile, slots, 3 * product_us(q), 128.0 * wgs * q.d * 4e-6) : 1;
-  if (wgs * p.splits < enough) {
+  p.splits = rows > 64 || wgs >= enough ? cut(wgs, (q.M + tile - 1) / tile, slots, 3 * product_us(q), 128.0 * wgs * q.d * 4e-6) : 1;
+  if (wgs * p.splits < enough || (rows <= few && q.M >= 4 * joined)) {
+    const long long n = heads * ((rows + 31) / 32);
     p.join = 1;
-    p.splits = pieces_joined(heads * ((rows + 31) / 32), (q.M + joined - 1) / joined);
+    p.splits = pieces_joined(n, (q.M + joined - 1) / joined, 32.0 * n * q.d * 4e-6);
   }
   p.row_tile = p.join ? 32 : 128;
   p.tiles = (int)((rows + p.row_tile - 1) / p.row_tile);
   const int stretches = dense_packed(q) ? 1 : q.group;   // a piece stays within the rows of a head
   wgs = kv_heads * stretches * ((q.M + 127) / 128);
   p.kv_join = 0;
-  p.per_head = q.M > 64 ? cut(wgs, (rows + tile - 1) / tile, slots, 4 * product_us(q), 2.0 * kv_heads * q.M * q.d * 4e-6) : 1;
+  const double kv_mb = 2.0 * kv_heads * q.M * q.d * 4e-6;
+  p.per_head = q.M > 64 || wgs >= enough ? cut(wgs, (rows + tile - 1) / tile, slots, 4 * product_us(q), kv_mb) : 1;
   const size_t tiles_lds = 2 * (2 * (size_t)joined * row_bytes + 1024);
-  if (wgs * p.per_head < enough && tiles_lds + dkv_bias_lds(q, row_bytes > 256 ? 2 : 4) <= kLds) {
+  if ((wgs * p.per_head < enough || (q.M <= few && rows >= 4 * joined)) && tiles_lds + dkv_bias_lds(q, row_bytes > 256 ? 2 : 4) <= kLds) {
     p.kv_join = 1;
-    p.per_head = pieces_joined(kv_heads * stretches * ((q.M + 31) / 32), (rows + joined - 1) / joined);
+    p.per_head = pieces_joined(kv_heads * stretches * ((q.M + 31) / 32), (rows + joined - 1) / joined, kv_mb);
   }
   const int kt = p.kv_join ? 32 : 128;
   p.q_tile = p.kv_join ? joined : kv_tile;

@@ -1,12 +1,26 @@
-"""Dense attention: which kernel runs for what (the launches are noted, nothing runs)."""
+"""Dense attention: which kernel runs for what (the launches are noted, nothing runs).  test_gpu_dense_kernels.py runs the same problems."""
 import os
 
 import pytest
 
-from dense_kernels import RULE, TYPES, record
+from dense_kernels import RULE, SHAPES, TYPES, cases, problem, record, wanted
 from paper_2505_14708_amd import binding as da
 
 pytestmark = pytest.mark.skipif(not os.path.exists(da.LIB_PATH), reason="library not built")
+
+
+def test_problems_reach_the_kernels_that_they_are_for(tmp_path):
+    """And all of them together reach every dense kernel that the library has."""
+    all_cases = cases()
+    known, calls = record(tmp_path, [problem(dtype, d, mode, *SHAPES[shape]) for shape, mode, dtype, d in all_cases])
+    assert len(calls) == len(all_cases)
+    seen = set()
+    for (shape, mode, dtype, d), call in zip(all_cases, calls):
+        got = {k for k, _ in call}
+        seen |= got
+        for k in wanted(shape, dtype, d, mode):
+            assert k in got, (shape, mode, dtype, d, k, sorted(got))
+    assert seen == known, f"not run: {sorted(known - seen)}"
 
 
 @pytest.mark.parametrize("rule", [None, RULE])

@@ -296,7 +296,8 @@ def _attn(what, p, bias, layouts, Q, K, V, table, kv_len, O, lse, ws, stream, gr
     torch, dtypes = _torch_dtypes
     L = lib()
     dt = dtypes.get(p.dtype)
-    plain = isinstance(Q, int) or Q is None                       # plain addresses: nothing to look at
+    # nothing but plain addresses: nothing to look at
+    plain = (isinstance(Q, int) or Q is None) and all(t is None or isinstance(t, int) for t in (K, V, table, kv_len, O, lse, ws, *(grads or ())))
     dev = -1 if plain else torch.cuda.current_device()
     B, H, Hk, N, M, d = p.B, p.H, p.Hk, p.N, p.M, p.d
     lq = lk = lv = lo = None
@@ -308,8 +309,8 @@ def _attn(what, p, bias, layouts, Q, K, V, table, kv_len, O, lse, ws, stream, gr
     o, l = _place(O, what, "O", rows, dt, lo, dev), _place(lse, what, "lse", (B, H, N), f32, None, dev)
     n = _place(kv_len, what, "kv_len", (B,), i32, None, dev)
     ws_at, ws_bytes = (ws, 2 ** 63) if ws is None or isinstance(ws, int) else (ws.data_ptr(), ws.numel() * ws.element_size())
-    if ws is not None and not isinstance(ws, int) and not plain and ws.get_device() != dev:
-        raise DaError(-2, f"{what}: ws is on device {ws.device}, the current device is {dev}")
+    if ws is not None and not isinstance(ws, int) and (ws.get_device() != dev or not ws.is_contiguous()):
+        raise DaError(-2, f"{what}: ws is on device {ws.device}, strides {ws.stride()}; expected contiguous memory on the current device, {dev}")
     s = torch.cuda.current_stream().cuda_stream if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
     P, Y = ctypes.byref(p), None if layouts is None else ctypes.byref(layouts)
     R, shape = None, None

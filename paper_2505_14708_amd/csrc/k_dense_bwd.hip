@@ -3,18 +3,20 @@
 // With x = scale q.k + bias, p = exp(x - lse), delta_i = dO_i . O_i and ds = p (dO.v - delta):
 //     dQ = scale ds K      dK = scale ds^T Q      dV = p^T dO      dtable[c] = sum of ds over the pairs whose bucket is c
 // Two kernels, each of which makes p and dO V^T anew (seven products of N x M x d instead of five, but no sums shared between
-// workgroups: no atomics, the same bits every time, and the sums stay in registers):
+// workgroups: no atomics, the same bits every time, and the sums stay in registers; bfloat16 has an eighth, p K):
 //   dense_dq_kernel   32 queries a wave on the lane axis, tiles of K and V pass by
 //   dense_dkv_kernel  32 keys a wave on the lane axis, tiles of Q and dO pass by, with lse and delta of their rows; also the sums for dtable
 // Where one side is short the other is cut and the pieces' sums are put together by a third launch, in a fixed order.
 //
-// delta.  O is stored with the type's rounding (bf16: 2^-8), and dO . O inherits it.  But sum_j ds_ij = 0 for the delta that belongs to p and
-// dO V^T, so what the first kernel's rows of ds add up to is what its delta is off by; the second kernel gets the corrected one.
-// (dtable, a sum of ds in which that error does not average out, was off by 2.9e-3 in norm with 64 heads of 512 by 512; by about its final
-// rounding's 1.7e-3 so.)
+// delta.  O is stored with the type's rounding (bfloat16: 2^-8), and dO . O inherits it.  But sum_j ds_ij = 0 for the delta that belongs to p and dO V^T,
+// so what the first kernel's rows of ds add up to is what its delta is off by.  Its dQ has that times the row's sum of p K too much, which in bfloat16 it
+// sums beside (dQ's error in norm, 512 keys, scores with a deviation of 1, 2, 4: 2.4e-3, 2.6e-3, 3.5e-3 without, 2.4e-3 with, which is what the roundings
+// of ds and dQ are; 24 heads of 32760 by 512, both gradient kernels: 785 us without, 840 with; a round over the keys for delta alone ahead of
+// the other would be 1040).  The second kernel, and dtable with it, gets the corrected delta.  (dtable was off by 2.9e-3 in norm with 64 heads of 512 by 512;
+// by about its final rounding's 1.7e-3 so.)
 //
-// Bounds: with 128 channels the matrix pipe at 0.8 to 0.97 PFLOP/s (24 heads of 32760 by 512: dQ 390 us, dK and dV 427 us), beside which the vector pipe
-// is busy about as long, with little of it at the same time; with 64 channels the vector instructions.
+// Bounds: with 128 channels the matrix pipe and LDS, beside which the vector pipe is busy about as long, with little of it at the same time; with 64
+// channels the vector instructions.
 #include <type_traits>
 #include "attn_tiles.h"
 
@@ -30,6 +32,7 @@ struct BwdArgs {
   float *start, *delta;            // [heads][padded rows]: where a row's scores start (start_of), -delta
   float *top, *log_l;              // the same: of rows in a far tile (kFarLse) the largest score and log2(sum) against it
   float *dq_part, *r_part, *dkv_part;  // sums of pieces: dQ, rows of ds, dK and dV
+  unsigned char* k_part;           // the same: scale p K, in bfloat16 (it is for a correction of some thousandths)
   float* bias_part;                // [work item][buckets]
   long long rows, padded;          // rows of a head as the kernels see them, and rounded up to 32
   long long items;                 // work items of the launch
@@ -113,11 +116,11 @@ template <class T> __device__ __forceinline__ bool is_far_lse(float l) { return 
 
 // The largest x (with a bias) or score (without) of each of the wave's 32 queries among all keys, and the sum of exp2(x - that), of waves that share
 // their queries a wave's part of both; through the first tile's memory, one tile at a time.
-template <class T, int D, int NW, int JW, int MODE>
+template <class T, int D, int KB, int NW, int JW, int MODE>
 __device__ __forceinline__ void far_sums(const DenseGeo& q, const Own<T, D> (&own)[1], const unsigned char* kb, long long ks, int len, int n_tiles,
                                          unsigned lds, unsigned s_lane, int wave, int lane, const float* bias_row, int first_row, int last_row,
                                          float& top, float& sum) {
-  constexpr int KB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>;
+  constexpr int RB = kRowBytes<T, D>;
   const int hi = lane >> 5;
   top = -FLT_MAX;
   sum = 0.f;
@@ -153,10 +156,18 @@ __device__ __forceinline__ void far_sums(const DenseGeo& q, const Own<T, D> (&ow
 
 template <class T, int D, int JW> constexpr int kDqWaves = JW > 1 || kRowBytes<T, D> > 256 ? 1 : 2;
 
+// bf16, 128 channels: the two sums are 128 registers, Q's and dO's rows 64 and the two squares 32, of 256.  With a bias 20 would be spilled; there dO's rows are
+// in LDS, 8 KB a wave, and the tiles of 32 rows so that two workgroups still fit a CU (24 heads of 4099 by 4099, both gradient kernels: 950 us
+// spilled, 916 so; without a bias, 24 heads of 32760 by 512, 840 and 860 us).
+template <class T, int D, int JW, int MODE> constexpr bool kGradInLds = sizeof(T) == 2 && D == 128 && JW == 1 && MODE == BIAS;
+template <class T, int D, int JW, int MODE> constexpr int kDqRows = kGradInLds<T, D, JW, MODE> ? 32 : kTileRows<T, D, JW>;
+
 template <class T, int D, int NW, int JW, int MODE>
 __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel(DenseGeo q, BwdArgs g) {
-  constexpr int KB = kTileRows<T, D, JW>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * (NW / JW);
-  __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * TILE];
+  constexpr int KB = kDqRows<T, D, JW, MODE>, RB = kRowBytes<T, D>, TILE = KB * RB, RT = 32 * (NW / JW);
+  constexpr bool GRAD_IN_LDS = kGradInLds<T, D, JW, MODE>;
+  constexpr int NZ = sizeof(T) == 2 ? 2 : 1;           // sums of ds K; of p K
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[4 * TILE + (GRAD_IN_LDS ? NW * 32 * RB : 0)];
   __shared__ float parts[NW * 32];
   extern __shared__ __attribute__((aligned(16))) float bias_row[];
   const long long id = blockIdx.y * (long long)gridDim.x + blockIdx.x;
@@ -190,7 +201,7 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
   if constexpr (MODE == BIAS) fill_bias<T>(bias_row, q.rule, (const T*)g.table, q.H, hd, threadIdx.x, 64 * NW);
 
   Own<T, D> own[1], grad[1];
-  f32x16 z[1][D / 32];
+  f32x16 z[NZ][D / 32];
   own[0].load(g.Q + query_offset<MODE>(q, q.q, b, hd, rc) * (long long)sizeof(T), hi);
   grad[0].load(g.dO + query_offset<MODE>(q, q.dout, b, hd, rc) * (long long)sizeof(T), hi);
   float delta = 0.f;
@@ -200,6 +211,10 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
 #pragma unroll
     for (int t = 0; t < Own<T, D>::N; ++t) delta = dot_piece<T>(grad[0].x[t], out.x[t], delta);
     delta = sum_across_halves(delta);
+    if constexpr (GRAD_IN_LDS) {
+#pragma unroll
+      for (int t = 0; t < Own<T, D>::N; ++t) *(bf16x8*)(tiles + 4 * TILE + wave * 32 * RB + t * 1024 + lane * 16) = grad[0].x[t];
+    }
   }
   float lse2 = rr <= last_row && l != -INFINITY ? l * kLog2e : INFINITY;   // far: log2(sum)
   bool far = false;                // the same for all waves of the workgroup
@@ -207,19 +222,17 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
   far = __builtin_amdgcn_readfirstlane(__any(far));
   float off = 0.f;                 // this lane's part of the row's sum of ds
 #pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt) z[0][dt] = zero16();
+  for (int n = 0; n < NZ; ++n)
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) z[n][dt] = zero16();
   const unsigned s_lane = scores_lane<T, D>(lane), m_lane = mix_lane<T, D>(lane);
   const unsigned bias_lds = MODE == BIAS ? (unsigned)(uintptr_t)(lds_f32*)bias_row : 0u;
 
-  // Few keys, all of them in the two pairs of buffers: one round for the sum of ds alone, from which delta is corrected, before the round for dQ.
-  // (dQ's error in norm with 4 to 31 keys 2.5e-3 to 3.8e-3 without, the roundings of ds and dQ 2.4e-3.  Over many keys what delta is off by
-  // hardly shows.)
-  const bool exact = g.splits == 1 && n_tiles <= 2;
   float top = 0.f;
   if (__builtin_expect(far, 0)) {
     wait_loads();
     float sum;
-    far_sums<T, D, NW, JW, MODE>(q, own, kb, ks, len, n_tiles, lds, s_lane, wave, lane, bias_row, first_row, last_row, top, sum);
+    far_sums<T, D, KB, NW, JW, MODE>(q, own, kb, ks, len, n_tiles, lds, s_lane, wave, lane, bias_row, first_row, last_row, top, sum);
     if constexpr (JW > 1) {
       if (hi == 0) parts[wave * 32 + lane] = top;
       __syncthreads();
@@ -243,85 +256,91 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
       load_tile<T, D, KB, NW>(vb, vs, t0 * KB, len - 1, lds + TILE, wave);
     }
   }
-  for (int round = exact ? 0 : 1; round < 2; ++round) {
-    for (int t = t0; t < t1; ++t) {
-      const unsigned buf = lds + ((t - t0) & 1) * (2 * TILE);
-      wait_loads();
-      tile_barrier();
-      if (t + 1 < t1 && !(exact && round == 1)) {
-        const unsigned next = lds + ((t + 1 - t0) & 1) * (2 * TILE);
-        load_tile<T, D, KB, NW>(kb, ks, (t + 1) * KB, len - 1, next, wave);
-        load_tile<T, D, KB, NW>(vb, vs, (t + 1) * KB, len - 1, next + TILE, wave);
-      }
-      if (first_row > last_row) continue;
+  for (int t = t0; t < t1; ++t) {
+    const unsigned buf = lds + ((t - t0) & 1) * (2 * TILE);
+    wait_loads();
+    tile_barrier();
+    if (t + 1 < t1) {
+      const unsigned next = lds + ((t + 1 - t0) & 1) * (2 * TILE);
+      load_tile<T, D, KB, NW>(kb, ks, (t + 1) * KB, len - 1, next, wave);
+      load_tile<T, D, KB, NW>(vb, vs, (t + 1) * KB, len - 1, next + TILE, wave);
+    }
+    if (first_row > last_row) continue;
 #pragma unroll
-      for (int i = 0; i < KB / 32 / JW; ++i) {
-        const int sub = JW > 1 ? wave : i;
-        const int key0 = t * KB + 32 * sub;
-        if (key0 >= len) break;
-        f32x16 s[1], dp[1];
-        scores<T, D, 1>(buf + sub * 32 * RB + s_lane, own, s);
+    for (int i = 0; i < KB / 32 / JW; ++i) {
+      const int sub = JW > 1 ? wave : i;
+      const int key0 = t * KB + 32 * sub;
+      if (key0 >= len) break;
+      f32x16 s[1], dp[1];
+      scores<T, D, 1>(buf + sub * 32 * RB + s_lane, own, s);
+      if constexpr (GRAD_IN_LDS) {
+        dp[0] = zero16();
+        add_scores_lds<D>(buf + TILE + sub * 32 * RB + s_lane, lds + 4 * TILE + wave * 32 * RB + lane * 16, dp[0]);
+      } else {
         scores<T, D, 1>(buf + TILE + sub * 32 * RB + s_lane, grad, dp);
-        const int left = len - key0 - 8 * hi;
-        if constexpr (MODE == BIAS) {
-          const int low = key0 - first_row - q.q_pos;          // r of key 0 and query 0 of the square
-          if (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut) {
-            const float out = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
-            if (__builtin_expect(far, 0)) {
+      }
+      const int left = len - key0 - 8 * hi;
+      if constexpr (MODE == BIAS) {
+        const int low = key0 - first_row - q.q_pos;          // r of key 0 and query 0 of the square
+        if (low - 31 >= q.rule.cut || low + 31 <= -q.rule.cut) {
+          const float out = bias_row[low > 0 ? 2 * (q.rule.cut + kBiasPad) : 0];
+          if (__builtin_expect(far, 0)) {
 #pragma unroll
-              for (int a = 0; a < 16; ++a) s[0][a] = exp2_fast((biased<T>(q, s[0][a], out) - top) - lse2);
-            } else {
-#pragma unroll
-              for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], out - lse2);
-            }
+            for (int a = 0; a < 16; ++a) s[0][a] = exp2_fast((biased<T>(q, s[0][a], out) - top) - lse2);
           } else {
-            f32x16 bs;
-            read_bias<1>(bias_lds + 4 * (low + 8 * hi - (lane & 31) + q.rule.cut + kBiasPad), bs);
-            if (__builtin_expect(far, 0)) {
 #pragma unroll
-              for (int a = 0; a < 16; ++a) s[0][a] = exp2_fast((biased<T>(q, s[0][a], bs[a]) - top) - lse2);
-            } else {
-#pragma unroll
-              for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], bs[a] - lse2);
-            }
+            for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], out - lse2);
           }
         } else {
-          if (far || key0 + 32 > len) {
+          f32x16 bs;
+          read_bias<1>(bias_lds + 4 * (low + 8 * hi - (lane & 31) + q.rule.cut + kBiasPad), bs);
+          if (__builtin_expect(far, 0)) {
 #pragma unroll
-            for (int a = 0; a < 16; ++a) s[0][a] = 16 * (a >> 3) + (a & 7) < left ? s[0][a] - top : -INFINITY;
+            for (int a = 0; a < 16; ++a) s[0][a] = exp2_fast((biased<T>(q, s[0][a], bs[a]) - top) - lse2);
+          } else {
+#pragma unroll
+            for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], bs[a] - lse2);
           }
-#pragma unroll
-          for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], -lse2);
         }
-        if (MODE == BIAS && key0 + 32 > len) {
+      } else {
+        if (far || key0 + 32 > len) {
 #pragma unroll
-          for (int a = 0; a < 16; ++a) s[0][a] = 16 * (a >> 3) + (a & 7) < left ? s[0][a] : 0.f;
+          for (int a = 0; a < 16; ++a) s[0][a] = 16 * (a >> 3) + (a & 7) < left ? s[0][a] - top : -INFINITY;
         }
 #pragma unroll
-        for (int a = 0; a < 16; ++a) {
-          s[0][a] *= dp[0][a] - delta;
-          off += s[0][a];
-        }
-        if (round == 0) continue;
-        const Mixed<T> ds[1] = {Mixed<T>(s[0])};
-        mix<T, D, 1>(buf + sub * 32 * RB + m_lane, ds, z);
+        for (int a = 0; a < 16; ++a) s[0][a] = power_of<T>(q, s[0][a], -lse2);
       }
-    }
-    if (round == 0) {
-      off = sum_across_halves(off);
-      if constexpr (JW > 1) {
-        if (hi == 0) parts[wave * 32 + lane] = off;
-        __syncthreads();
-        off = 0.f;
+      if (MODE == BIAS && key0 + 32 > len) {
 #pragma unroll
-        for (int w = 0; w < NW; ++w) off += parts[w * 32 + (lane & 31)];
+        for (int a = 0; a < 16; ++a) s[0][a] = 16 * (a >> 3) + (a & 7) < left ? s[0][a] : 0.f;
       }
-      delta += off;
-      off = 0.f;
+      Mixed<T> c[NZ];
+      if constexpr (NZ == 2) c[1] = Mixed<T>(s[0]);
+#pragma unroll
+      for (int a = 0; a < 16; ++a) {
+        s[0][a] *= dp[0][a] - delta;
+        off += s[0][a];
+      }
+      c[0] = Mixed<T>(s[0]);
+      mix<T, D, NZ>(buf + sub * 32 * RB + m_lane, c, z);
     }
   }
   off = sum_across_halves(off);
+  if constexpr (JW > 1) {
+    if (hi == 0) parts[wave * 32 + lane] = off;
+    __syncthreads();
+    off = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) off += parts[w * 32 + (lane & 31)];
+  }
   const bool there = rr <= last_row;
+  const float f = g.splits == 1 ? off : 0.f;           // (pieces: dense_sum_dq_kernel)
+  if constexpr (NZ == 2) {
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int a = 0; a < 16; ++a) z[0][dt][a] = __builtin_fmaf(z[1][dt][a], -f, z[0][dt][a]);
+  }
   if constexpr (JW > 1) {
     float* buf = (float*)tiles;
     join_waves<D, NW>(buf, wave, lane, z[0], q.scale, [&](int row, int c, f32x4 (&x)[2]) {
@@ -329,11 +348,12 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
       if (g.splits == 1) store8<T>(g.dQ + (query_offset<MODE>(q, q.dq, b, hd, first_row + row) + c) * (long long)sizeof(T), x, 1.f);
       else store8<float>((unsigned char*)(g.dq_part + (item * RT + row) * D + c), x, 1.f);
     });
-    if (hi == 0) parts[wave * 32 + lane] = off;
-    __syncthreads();
-    off = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) off += parts[w * 32 + (lane & 31)];
+    if constexpr (NZ == 2) {
+      if (g.splits > 1)
+        join_waves<D, NW>(buf, wave, lane, z[1], q.scale, [&](int row, int c, f32x4 (&x)[2]) {
+          if (first_row + row <= last_row) store8<T>(g.k_part + ((item * RT + row) * D + c) * (long long)sizeof(T), x, 1.f);
+        });
+    }
     if (wave != 0) return;
     if (g.splits > 1 && there && hi == 0) g.r_part[item * RT + lane] = off;
   } else if (g.splits == 1) {
@@ -341,6 +361,7 @@ __global__ __launch_bounds__(64 * NW, (kDqWaves<T, D, JW>)) void dense_dq_kernel
   } else {
     const long long at = item * RT + wave * 32 + (lane & 31);
     store_column<float, D>((unsigned char*)(g.dq_part + at * D), hi, z[0], q.scale, there);
+    if constexpr (NZ == 2) store_column<T, D>(g.k_part + at * RB, hi, z[1], q.scale, there);
     if (there && hi == 0) g.r_part[at] = off;
   }
   if (split == 0 && hi == 0 && rr < g.padded) {
@@ -609,16 +630,22 @@ __global__ __launch_bounds__(256) void dense_sum_dq_kernel(DenseGeo q, BwdArgs g
   const int heads = heads_of<MODE>(q);
   if (row >= (long long)q.B * heads * g.rows) return;
   const long long bh = row / g.rows;
-  const int rr = (int)(row - bh * g.rows), b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads);
+  const int rr = (int)(row - bh * g.rows), b = (int)(bh / heads), hd = (int)(bh - (long long)b * heads), c = threadIdx.x % P;
   const int tile = rr / RT;
   const long long first = ((bh * g.tiles + tile) * g.splits) * RT + (rr - tile * RT);
-  sum_pieces<T, D>(g.dq_part + first * D, (long long)RT * D, g.splits, (T*)g.dQ + query_offset<MODE>(q, q.dq, b, hd, rr), threadIdx.x % P);
-  if (threadIdx.x % P == 0) {      // and what delta is off by
-    float off = 0.f;
+  T* out = (T*)g.dQ + query_offset<MODE>(q, q.dq, b, hd, rr) + 4 * c;
+  float off = 0.f;                 // what delta is off by
+  f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int s = 0; s < g.splits; ++s) off += g.r_part[first + (long long)s * RT];
-    g.delta[bh * g.padded + rr] -= off;
+  for (int s = 0; s < g.splits; ++s) {
+    const long long at = first + (long long)s * RT;
+    off += g.r_part[at];
+    x += *(const f32x4*)(g.dq_part + at * D + 4 * c);
+    if constexpr (sizeof(T) == 2) y += __builtin_convertvector(*(const bf16x4*)(g.k_part + (at * D + 4 * c) * 2), f32x4);
   }
+  if constexpr (sizeof(T) == 2) *(bf16x4*)out = __builtin_convertvector(x - y * off, bf16x4);
+  else *(f32x4*)out = x;
+  if (c == 0) g.delta[bh * g.padded + rr] -= off;
 }
 
 template <class T, int D>
@@ -672,7 +699,7 @@ constexpr size_t kLds = 160 * 1024;
 struct BwdPlan {
   int join, row_tile, tiles, splits;                                            // dq
   int kv_join, kv_tiles, kv_splits, per_head, row_tiles, q_tile;                // dkv
-  size_t start, delta, top, log_l, dq_part, r_part, dkv_part, bias_part, total;
+  size_t start, delta, top, log_l, k_part, dq_part, r_part, dkv_part, bias_part, total;
 };
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -737,6 +764,7 @@ BwdPlan plan_bwd(const DenseGeo& q) {
   p.top = off; off += align_up(heads * padded * sizeof(float));
   p.log_l = off; off += align_up(heads * padded * sizeof(float));
   p.dq_part = off; off += p.splits > 1 ? align_up((size_t)heads * p.tiles * p.splits * p.row_tile * q.d * sizeof(float)) : 0;
+  p.k_part = off; off += p.splits > 1 && !f32 ? align_up((size_t)heads * p.tiles * p.splits * p.row_tile * q.d * 2) : 0;
   p.r_part = off; off += p.splits > 1 ? align_up((size_t)heads * p.tiles * p.splits * p.row_tile * sizeof(float)) : 0;
   p.dkv_part = off; off += p.kv_splits > 1 ? align_up(2 * (size_t)p.kv_splits * kv_heads * q.M * q.d * sizeof(float)) : 0;
   p.bias_part = off; off += q.bias ? align_up((size_t)kv_heads * p.kv_tiles * p.kv_splits * q.buckets * sizeof(float)) : 0;
@@ -800,6 +828,7 @@ hipError_t launch_dense_bwd(const DenseGeo& q, const void* Q, const void* K, con
   a.top = (float*)(base + p.top); a.log_l = (float*)(base + p.log_l);
   a.dq_part = (float*)(base + p.dq_part); a.r_part = (float*)(base + p.r_part); a.dkv_part = (float*)(base + p.dkv_part);
   a.bias_part = (float*)(base + p.bias_part);
+  a.k_part = (unsigned char*)(base + p.k_part);
   a.rows = dense_rows(q);
   a.padded = (a.rows + 31) / 32 * 32;
   a.tiles = a.splits = a.per_head = a.row_tiles = 0;

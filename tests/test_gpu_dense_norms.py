@@ -8,7 +8,7 @@ delta from the stored O and nothing else adds about as much again where the scor
 import pytest
 import torch
 
-from dense_util import Problem
+from dense_util import Problem, bucket_map
 
 pytestmark = pytest.mark.gpu
 ROUNDING = 1.659e-3
@@ -36,3 +36,22 @@ def test_table(d):
     pr = Problem("bf16", 1, 64, 64, 512, 512, d, rule=(32, 128, 1, 0), scale=d ** -0.5, seed=5)
     off = norms(pr, ("dtable", "dk"))
     assert off["dtable"] < 1.25 * ROUNDING and off["dk"] < 1.05 * 2.0 ** 0.5 * ROUNDING, off
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gain", [1.0, 2.0, 4.0])
+@pytest.mark.parametrize("heads,rows,keys,rule", [(16, 512, 130, None), (16, 512, 512, None), (16, 512, 2000, None), (16, 40, 3000, None), (64, 300, 300, None),
+                                                  (16, 512, 512, (32, 128, 1, 0))])
+def test_gradient_of_queries(d, gain, heads, rows, keys, rule):
+    """dQ is off by what the roundings of ds and of dQ make of the values in 64 bits here, with any number of keys, in one piece or several."""
+    pr = Problem("bf16", 1, heads, heads, rows, keys, d, gain=gain, rule=rule, scale=d ** -0.5, seed=7)
+    off = norms(pr, ("dq",))["dq"]
+    q, k, v, do = (pr.t[n][0].double() for n in ("q", "k", "v", "do"))
+    x = pr.scale * (q @ k.transpose(1, 2).contiguous())
+    if rule:
+        x = x + pr.table.double().t()[:, bucket_map(rows, keys, rule).cuda()]
+    p, dp = torch.softmax(x, 2), do @ v.transpose(1, 2).contiguous()
+    ds = p * (dp - (p * dp).sum(2, keepdim=True))
+    dq = pr.scale * (ds @ k)
+    least = float(((pr.scale * (ds.bfloat16().double() @ k)).bfloat16().double() - dq).norm() / dq.norm())
+    assert off < 1.05 * least, (off, least)

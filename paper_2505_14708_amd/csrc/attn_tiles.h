@@ -454,7 +454,8 @@ inline int cut(long long wgs, long long units, int slots, double unit_us, double
   }
   return best;
 }
-// us of a tile for one product, two workgroups of four waves to a CU: bf16 64 rows, float32 64 rows of 64 or 32 of 128 channels
+// us of a tile for one product, two workgroups of four waves to a CU (as all rules count; with 64 channels registers and LDS let in three to five of
+// some kernels): bf16 64 rows, float32 64 rows of 64 or 32 of 128 channels
 inline double product_us(const DenseGeo& q) { return q.dtype == DA_F32 ? 3.4 : q.d == 128 ? 0.85 : 0.5; }
 
 }  // namespace da

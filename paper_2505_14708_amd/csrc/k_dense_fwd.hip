@@ -4,8 +4,9 @@
 // two products of attn_tiles.h; the queries lie on the lane axis.  Tiles of K and V come through LDS, twice buffered and shared by the waves
 // of the workgroup.
 //
-// Bounds: 40 heads of 75600 by 512, 128 channels, bf16: 865 us, 0.92 PFLOP/s (a large library product reaches 1.22 on this card); the matrix pipe is busy
-// 39 % and the vector pipe 46 % of the cycles, with little of it at the same time.  One query of 32768 keys at 32 heads: K and V at 4.5 TB/s.
+// Bounds: 40 heads of 75600 by 512, 128 channels, bf16: 866 us, 0.92 PFLOP/s (a large library product reaches 1.23 on this card); in a counted run of 980 us the
+// matrix pipe is busy 42 % and the vector pipe 50 % of the cycles, with little of it at the same time, LDS 10 %.  One query of 32768 keys at 32 heads: K and V at
+// 4.5 TB/s.
 #include <type_traits>
 #include "attn_tiles.h"
 

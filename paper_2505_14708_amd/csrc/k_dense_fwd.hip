@@ -302,22 +302,28 @@ hipError_t pick_fwd(const DenseGeo& q, const FwdPlan& p, const dense::FwdArgs& a
 }  // namespace
 
 // Workgroups of four waves with 64 queries each (bf16, where they fill the card: each operand from LDS feeds two products), with 32 each, or of
-// waves that share 32 queries and take the keys in turn.
+// waves that share 32 queries and take the keys in turn: where there are few workgroups, and, with at most 64 queries, where those that join fit the card at once or, with
+// 64 channels, their tiles of 128 keys are several.  (192 heads of 16 queries by 2000 keys, bf16, 128 channels: joining 36 us, else 56, in two pieces 38; 960
+// heads: 182 and 171; of 64 queries by 64 keys 46 and 17.  float32, 64 channels, 960 heads of 16 by 2000: 273 and 386, by 64 keys 27 and 22; bf16, 64 channels,
+// 384 heads of 64 by 2000: 41 and 49, by 300 keys 13 and 11; 720 heads by 2000 91 and 71.)
 FwdPlan plan_dense_fwd(const DenseGeo& q) {
   FwdPlan p;
   const long long rows = dense_rows(q), heads = (long long)q.B * dense_heads(q);
   const bool f32 = q.dtype == DA_F32, wide = q.d * (f32 ? 4 : 2) > 256;
   const long long wgs = heads * ((rows + 127) / 128), units = (q.M + (wide ? 31 : 63)) / (wide ? 32 : 64);
+  const long long small = heads * ((rows + 31) / 32);
+  const int enough = kCUs / 4 * 3, slots = q.d * (f32 ? 4 : 2) == 128 ? 2 * kCUs : kCUs;     // (of workgroups that join)
   p.join = 0; p.sets = 1; p.splits = 1;
   if (!f32 && rows > 128 && heads * ((rows + 255) / 256) >= kCUs / 2 * 3) {   // three quarters of the places, two to a CU
     p.sets = 2;
-  } else if (wgs < kCUs / 4 * 3 || rows <= 64) {
-    p.splits = rows > 64 ? cut(wgs, units, 2 * kCUs, 2 * product_us(q), 128.0 * wgs * q.d * 4e-6) : 1;
-    if (wgs * p.splits < kCUs / 4 * 3 || rows <= 64) {
+  } else if (wgs < enough || rows <= 64) {
+    p.splits = rows > 64 || wgs >= enough ? cut(wgs, units, 2 * kCUs, 2 * product_us(q), 128.0 * wgs * q.d * 4e-6) : 1;
+    const bool many_keys = q.d == 64 && (f32 ? q.M >= 256 : rows <= 32 ? q.M >= 512 : q.M >= 1000 && small <= 2 * slots);
+    if (wgs * p.splits < enough || (rows <= 64 && (small <= slots || many_keys))) {
       p.join = 1;
-      const int n = wide ? 64 : 128, slots = q.d * (f32 ? 4 : 2) == 128 ? 2 * kCUs : kCUs;
-      const long long small = heads * ((rows + 31) / 32), tiles = (q.M + n - 1) / n;
-      long long s = small > 0 ? slots / small : 1;
+      const int n = wide ? 64 : 128;
+      const long long tiles = (q.M + n - 1) / n;
+      long long s = slots / small;
       if (s > tiles / 2) s = tiles / 2;
       p.splits = s < 1 ? 1 : (int)s;
     }

@@ -79,7 +79,7 @@ def problem(dtype, d, mode, heads, rows, M):
 # heads, rows, keys: what they stand for
 SHAPES = {"two sets": (400, 130, 70), "own columns": (200, 100, 140), "joining": (2, 62, 75), "few rows, cut": (2, 4, 3000),
           "cut": (20, 110, 3000), "many rows, cut": (2, 3000, 70), "many rows, few columns": (2, 3000, 20), "heads, many rows": (100, 2100, 65),
-          "heads, few columns": (192, 4200, 16), "heads, few rows": (192, 16, 4200)}
+          "heads, few columns": (192, 4200, 16), "heads, few rows": (192, 16, 4200), "many heads, few rows": (600, 40, 70)}
 
 
 def wanted(shape, dtype, d, mode):
@@ -98,7 +98,8 @@ def wanted(shape, dtype, d, mode):
             "many rows, few columns": [("dkv", *t, j, j, m), ("sum_dkv", *t)] if packs else [],
             "heads, many rows": [("fwd", *t, 2 if two else 1, 4, 1, m), ("dkv", *t, 4, 1, m)] if packs else [],
             "heads, few columns": [("dkv", *t, *few, m), ("sum_dkv", *t)] if packs else [],
-            "heads, few rows": [("fwd", *t, 1, j, j, m), ("dq", *t, *few, m), ("sum_dq", *t, m)]}[shape]
+            "heads, few rows": [("fwd", *t, 1, j, j, m), ("dq", *t, *few, m), ("sum_dq", *t, m)],
+            "many heads, few rows": [("fwd", *t, 1, 4, 1, m), ("dq", *t, 4, 1, m)]}[shape]
 
 
 def cases():

@@ -117,3 +117,27 @@ def test_rows_that_only_large_negative_entries_reach(dtype, d, low):
             x.masked_fill_(torch.arange(M, device="cuda") >= pr.lens[:, None, None, None], -math.inf)
         # scores of scale q.k below 1e-6 * 128 * 5: a factor of 1 + 2^-10 at most
         check(pr.results(), gradients(pr, torch.softmax(x, 3), 2.0 ** -10 + 2 * M * E, which), where)
+
+
+@pytest.mark.parametrize("rule", [None, (8, 16, 1, 0)])
+def test_captured_and_replayed_with_scores_of_either_size(rule):
+    """One graph, replayed with ordinary queries and with ones whose scores are large, between eager calls: the eager call's bits."""
+    pr = Problem("bf16", 2, 4, 4, 140, 1000, 64, rule=rule, lens=[1000, 90], seed=9)
+    ordinary, large = pr.t["q"].clone(), pr.t["q"] * 1e7
+    pr.run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        pr.run()
+    for i, q in enumerate((large, ordinary, large, ordinary)):
+        pr.t["q"].copy_(q)
+        pr.run()
+        shares(pr, f"replay {i} {rule}")
+        want = {n: x.clone() for n, x in pr.results().items()}
+        for x in pr.results().values():
+            x.fill_(5.0)
+        pr.ws.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        for n, x in pr.results().items():
+            assert torch.equal(x, want[n]), (rule, i, n)
